@@ -59,7 +59,8 @@ extern "C" void rh_destroy(rh_ctx* ctx)
     void* ptrs[] = {ctx->w_f32, ctx->wpack, ctx->bpack, ctx->fold_w, ctx->fold_b, ctx->frame_seg, ctx->seg_par, ctx->seg_T, ctx->seg_budget,
                     ctx->frame_nsel, ctx->frame_ties, ctx->owner_id, ctx->rank_of_id, ctx->raw, ctx->sorted,
                     ctx->pcount, ctx->tr_off, ctx->tr_A, ctx->tr_T, ctx->act,
-                    ctx->cell_mark, ctx->cell_live, ctx->cell_dead, ctx->cell_cnt, ctx->need_dmin, ctx->need_lists, ctx->need_cnt};
+                    ctx->cell_mark, ctx->cell_live, ctx->cell_dead, ctx->cell_cnt, ctx->need_dmin, ctx->need_lists, ctx->need_cnt,
+                    ctx->seq_ws, ctx->seq_cnt};
     for (void* p : ptrs) if (p) (void)hipFree(p);
     if (ctx->lost) (void)hipHostFree((void*)ctx->lost);
     delete ctx;

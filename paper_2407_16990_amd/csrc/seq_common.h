@@ -1,0 +1,54 @@
+// Shared by the operators of include/rh_seq.h.
+#pragma once
+#include "rh_internal.h"
+#include "rh_seq.h"
+
+#define SEQ_E4M3_MAX 448.0f
+#define SEQ_AMAX_MIN 0x1p-100f           // smaller largest magnitudes share a scale, so that its inverse stays finite
+
+typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 bf16x8;
+typedef __attribute__((__vector_size__(4 * sizeof(float)))) float f32x4;
+
+__device__ __forceinline__ float seq_bf16_lo(uint32_t u) { return __uint_as_float(u << 16); }
+__device__ __forceinline__ float seq_bf16_hi(uint32_t u) { return __uint_as_float(u & 0xFFFF0000u); }
+__device__ __forceinline__ uint32_t seq_pack_bf16(float a, float b)
+{
+    typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf16x2;
+    typedef __attribute__((__vector_size__(2 * sizeof(float)))) float f32x2;
+    const f32x2 v = {a, b};
+    const bf16x2 r = __builtin_convertvector(v, bf16x2);     // round to nearest even
+    return *(const uint32_t*)&r;
+}
+// four floats to e4m3, rounded to nearest even (magnitudes up to 448 and a rounding error above)
+__device__ __forceinline__ uint32_t seq_pack_e4m3(float a, float b, float c, float d)
+{
+    int r = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, r, true);
+}
+
+// A vector in memory that need not be aligned: global loads and stores take any byte address, and one instruction
+// that crosses a line costs less than one for every element.
+template <typename V> struct __attribute__((packed, aligned(1))) seq_loose { V v; };
+template <typename V> __device__ __forceinline__ V seq_load(const void* p) { return ((const seq_loose<V>*)p)->v; }
+template <typename V> __device__ __forceinline__ void seq_store(void* p, V v) { ((seq_loose<V>*)p)->v = v; }
+
+__device__ __forceinline__ float seq_to_f32(float v) { return v; }
+__device__ __forceinline__ float seq_to_f32(__bf16 v) { return (float)v; }
+__device__ __forceinline__ float seq_to_f32(uint8_t v) { return __builtin_amdgcn_cvt_f32_fp8((int)v, 0); }
+
+// A whole division by a number that is fixed for the launch: floor(x / d) for 0 <= x < 2^31, by the high half of a product.
+// With 2^s < d <= 2^(s+1) and m = ceil(2^(32+s) / d) < 2^32, x*m / 2^(32+s) passes x / d by less than x / 2^(32+s) < 2^-(s+1) <= 1 / d:
+// the floor is right.  d = 1 goes without.
+struct seq_div { uint32_t d, m, s; };
+inline seq_div seq_make_div(uint32_t d)
+{
+    if (d <= 1) return {1, 0, 0};
+    uint32_t s = 31 - (uint32_t)__builtin_clz(d - 1);        // 2^s <= d - 1 < 2^(s+1)
+    return {d, (uint32_t)(((1ull << (32 + s)) + d - 1) / d), s};
+}
+__device__ __forceinline__ uint32_t seq_quot(uint32_t x, const seq_div& v) { return v.d == 1 ? x : __umulhi(x, v.m) >> v.s; }
+
+// scratch memory of rh_cache_attend: partial results, and counters that are zero between calls
+rh_status seq_ensure(rh_ctx* ctx, size_t bytes, size_t counters);
+// refusals of a cache; `name` is the call's
+rh_status seq_check_cache(rh_ctx* ctx, const char* name, const rh_kv_cache* c);
