@@ -12,8 +12,8 @@
  * stream, arguments checked before any launch, rh_last_error.  They use neither the context's network nor its capacities,
  * and count in no class of rh_profile_read.  Sums, softmax statistics and norms are held in 32 bits.
  * Scratch memory of rh_cache_attend belongs to the context and only grows: a call that needs more than every earlier one
- * synchronises the stream and reallocates it; what it needs follows from n_streams, heads and dim alone, not from the lengths, so that
- * after one call a graph of calls of the same sizes may be captured.  The others need none.
+ * synchronises the stream and reallocates it; what it needs follows from the head size alone, so that after one call a graph of calls
+ * with heads as large may be captured.  rh_cache_plan has a counter there, which any first call of either makes.  The others need none.
  */
 #ifndef RH_SEQ_H
 #define RH_SEQ_H

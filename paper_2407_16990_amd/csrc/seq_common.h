@@ -8,6 +8,7 @@
 
 typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 bf16x8;
 typedef __attribute__((__vector_size__(4 * sizeof(float)))) float f32x4;
+typedef __attribute__((__vector_size__(4 * sizeof(uint32_t)))) uint32_t u32x4;     // arrays of it stay in registers, where HIP's uint4 may not
 
 __device__ __forceinline__ float seq_bf16_lo(uint32_t u) { return __uint_as_float(u << 16); }
 __device__ __forceinline__ float seq_bf16_hi(uint32_t u) { return __uint_as_float(u & 0xFFFF0000u); }
@@ -26,6 +27,18 @@ __device__ __forceinline__ uint32_t seq_pack_e4m3(float a, float b, float c, flo
     return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, r, true);
 }
 
+// Inclusive running sum over the wave's lanes, by row shifts and row broadcasts of the vector ALU.
+__device__ __forceinline__ int32_t seq_scan(int32_t v)
+{
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);        // the last lane of rows 0 and 2 to rows 1 and 3
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);        // lane 31 to the upper half
+    return v;
+}
+
 // A vector in memory that need not be aligned: global loads and stores take any byte address, and one instruction
 // that crosses a line costs less than one for every element.
 template <typename V> struct __attribute__((packed, aligned(1))) seq_loose { V v; };
@@ -38,15 +51,15 @@ __device__ __forceinline__ float seq_to_f32(uint8_t v) { return __builtin_amdgcn
 
 // A whole division by a number that is fixed for the launch: floor(x / d) for 0 <= x < 2^31, by the high half of a product.
 // With 2^s < d <= 2^(s+1) and m = ceil(2^(32+s) / d) < 2^32, x*m / 2^(32+s) passes x / d by less than x / 2^(32+s) < 2^-(s+1) <= 1 / d:
-// the floor is right.  d = 1 goes without.
-struct seq_div { uint32_t d, m, s; };
+// the floor is right.  d = 1, whose m would not fit, goes by `one`, without a branch.
+struct seq_div { uint32_t d, m, s, one; };
 inline seq_div seq_make_div(uint32_t d)
 {
-    if (d <= 1) return {1, 0, 0};
-    uint32_t s = 31 - (uint32_t)__builtin_clz(d - 1);        // 2^s <= d - 1 < 2^(s+1)
-    return {d, (uint32_t)(((1ull << (32 + s)) + d - 1) / d), s};
+    if (d <= 1) return {1, 0, 0, ~0u};
+    const uint32_t s = 31 - (uint32_t)__builtin_clz(d - 1);  // 2^s <= d - 1 < 2^(s+1)
+    return {d, (uint32_t)(((1ull << (32 + s)) + d - 1) / d), s, 0};
 }
-__device__ __forceinline__ uint32_t seq_quot(uint32_t x, const seq_div& v) { return v.d == 1 ? x : __umulhi(x, v.m) >> v.s; }
+__device__ __forceinline__ uint32_t seq_quot(uint32_t x, const seq_div& v) { return (__umulhi(x, v.m) + (x & v.one)) >> v.s; }
 
 // scratch memory of rh_cache_attend: partial results, and counters that are zero between calls
 rh_status seq_ensure(rh_ctx* ctx, size_t bytes, size_t counters);
