@@ -55,14 +55,6 @@ template <int N> __device__ __forceinline__ void attend_get(uint32_t* to, const 
     else if constexpr (N == 2) { const uint2 u = *(const uint2*)from; to[0] = u.x; to[1] = u.y; }
     else { const uint4 u = *(const uint4*)from; to[0] = u.x; to[1] = u.y; to[2] = u.z; to[3] = u.w; }
 }
-// two e4m3 values of a word (its low or high half) as two bf16, which hold them exactly
-template <bool HIGH> __device__ __forceinline__ uint32_t attend_pair(uint32_t u)
-{
-    typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf16x2;
-    const bf16x2 r = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u, 1.0f, HIGH);
-    return *(const uint32_t*)&r;
-}
-
 template <int KIND, int D>
 __global__ __launch_bounds__(ATTEND_T) void k_seq_attend(attend_args a)
 {
@@ -236,7 +228,7 @@ __global__ __launch_bounds__(ATTEND_T) void k_seq_attend(attend_args a)
                     sc[tt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, ka), __builtin_bit_cast(bf16x8, qa), sc[tt], 0, 0, 0);
                 };
                 auto wide = [](uint32_t x, uint32_t y) {
-                    return attend_words<4>{attend_pair<false>(x), attend_pair<true>(x), attend_pair<false>(y), attend_pair<true>(y)};
+                    return attend_words<4>{seq_e4m3_pair<false>(x), seq_e4m3_pair<true>(x), seq_e4m3_pair<false>(y), seq_e4m3_pair<true>(y)};
                 };
 #pragma unroll
                 for (int s = 0; s < RB / 64; ++s) {
@@ -320,8 +312,8 @@ __global__ __launch_bounds__(ATTEND_T) void k_seq_attend(attend_args a)
                         uint32_t x, y;
                         if constexpr (KIND == RH_T_BF16) { x = vr[2 * w][i / 2]; y = vr[2 * w + 1][i / 2]; }
                         else {
-                            x = i & 2 ? attend_pair<true>(vr[2 * w][i / 4]) : attend_pair<false>(vr[2 * w][i / 4]);
-                            y = i & 2 ? attend_pair<true>(vr[2 * w + 1][i / 4]) : attend_pair<false>(vr[2 * w + 1][i / 4]);
+                            x = i & 2 ? seq_e4m3_pair<true>(vr[2 * w][i / 4]) : seq_e4m3_pair<false>(vr[2 * w][i / 4]);
+                            y = i & 2 ? seq_e4m3_pair<true>(vr[2 * w + 1][i / 4]) : seq_e4m3_pair<false>(vr[2 * w + 1][i / 4]);
                         }
                         even.w[w] = __builtin_amdgcn_perm(y, x, 0x05040100u);
                         odd.w[w] = __builtin_amdgcn_perm(y, x, 0x07060302u);

@@ -20,6 +20,13 @@ __device__ __forceinline__ uint32_t seq_pack_bf16(float a, float b)
     const bf16x2 r = __builtin_convertvector(v, bf16x2);     // round to nearest even
     return *(const uint32_t*)&r;
 }
+// two e4m3 values of a word (its low or high half) as two bf16, which hold them exactly
+template <bool HIGH> __device__ __forceinline__ uint32_t seq_e4m3_pair(uint32_t u)
+{
+    typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf16x2;
+    const bf16x2 r = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u, 1.0f, HIGH);
+    return *(const uint32_t*)&r;
+}
 // four floats to e4m3, rounded to nearest even (magnitudes up to 448 and a rounding error above)
 __device__ __forceinline__ uint32_t seq_pack_e4m3(float a, float b, float c, float d)
 {

@@ -1,4 +1,17 @@
 // rh_matvec_packed: products of a few rows with weights in 4 bits that share a scale by 32.
+//
+// Bound by the weights' bytes: a wave streams them from memory into the matrix operand, 16 outputs a product, and the rows x are the
+// other operand, out of LDS, where a workgroup lays them once for all the outputs that it goes through.  A lane's 16 bytes are the 32 codes of
+// one block, so that one scale byte goes with them.
+//   bf16 rows   8 codes at a time become bf16 values, their block's scale included (a conversion of the hardware; exact)
+//   fp32 rows   the same against x cut into three bf16 parts, which together are x exactly: products of full precision at three
+//               products of the 16-bit rate, where the fp32 rate is a sixteenth of it
+//   e4m3 rows   as bf16 rows, which hold them exactly; or the scaled product of 8-bit and 4-bit values, which takes codes, scales and rows
+//               as they are.  That one keeps fewer bits of its partial sums: against 64 bits, 2000 x 8 outputs of 32 / 512 / 8192 terms
+//               are 1.3e-6 / 3.5e-6 / 4.2e-6 off in norm, 0 / 3e-8 / 7e-8 as bf16 rows.  So it serves bf16 outputs only, whose
+//               rounding is 1.7e-3, and from one whole stretch of 512 terms on, where there is something to gain
+// A workgroup's waves share out its tiles of outputs and the inner index (KS waves a tile, summed in LDS in order), so that few outputs
+// still use every wave.
 #include "seq_common.h"
 
 struct matvec_args {
@@ -8,44 +21,347 @@ struct matvec_args {
     void* y;
     int64_t x_stride, y_stride;
     int32_t rows, outs, ins, blocks, relu;
+    int32_t tiles, ks, tw;       // tiles of outputs; waves a tile; tiles a workgroup at a time
+    int32_t quads, chunk;        // stretches of 512 of the inner index: all, and as many as x lies in LDS for at a time
+    int32_t y_f32;
 };
 
-__device__ __forceinline__ float matvec_scale(uint8_t s)
+#define MATVEC_WAVES 8
+#define MATVEC_LDS (160 * 1024)
+#define MATVEC_HUGE 252          // scales from here on can take a code past the largest bf16 number
+
+typedef __attribute__((__vector_size__(8 * sizeof(int)))) int i32x8;
+
+template <int XT> struct matvec_kind;
+template <> struct matvec_kind<RH_T_F32> { typedef float T; static constexpr int PARTS = 3, PIECE = 8; };
+template <> struct matvec_kind<RH_T_BF16> { typedef __bf16 T; static constexpr int PARTS = 1, PIECE = 8; };
+template <> struct matvec_kind<RH_T_E4M3> { typedef uint8_t T; static constexpr int PARTS = 1, PIECE = 8; };       // PIECE: elements of x in 16 bytes of LDS
+#define MATVEC_SCALED 3          // e4m3 rows on the scaled product
+template <> struct matvec_kind<MATVEC_SCALED> { typedef uint8_t T; static constexpr int PARTS = 1, PIECE = 16; };
+
+// x = the sum of three bf16 numbers, for any finite x: cut off, not rounded, so that none passes the largest
+__device__ __forceinline__ void matvec_cut(float x, uint32_t (&part)[3])
 {
-    return s == 255 ? __builtin_nanf("") : __uint_as_float(s ? (uint32_t)s << 23 : 0x00400000u);     // 2^(s - 127), 2^-127 below the normal numbers
-}
-__device__ __forceinline__ float matvec_code(uint32_t c)
-{
-    const uint32_t m = c & 7;
-    const float v = m < 2 ? 0.5f * (float)m : __uint_as_float((126 + (m >> 1)) << 23 | (m & 1) << 22);
-    return c & 8 ? -v : v;
+    const uint32_t u = __float_as_uint(x);
+    const bool finite = (u & 0x7F800000u) != 0x7F800000u;
+    part[0] = x != x ? 0x7FC0u : u >> 16;
+    const float r = finite ? x - __uint_as_float(u & 0xFFFF0000u) : 0.f;
+    part[1] = __float_as_uint(r) >> 16;
+    part[2] = __float_as_uint(r - __uint_as_float(__float_as_uint(r) & 0xFFFF0000u)) >> 16;
 }
 
-// One wave an output and row.
-template <typename T, typename Y>
-__global__ __launch_bounds__(256) void k_seq_matvec(matvec_args a)
+// 8 codes (the bytes of c, low half first) times 2^(scale - 127) as bf16
+__device__ __forceinline__ bf16x8 matvec_wide(uint32_t c, uint32_t scale)
 {
-    const int lane = threadIdx.x & 63, n = blockIdx.x * 4 + (threadIdx.x >> 6), m = blockIdx.y;
-    if (n >= a.outs) return;
-    const T* x = (const T*)a.x + m * a.x_stride;
-    float sum = 0.f;
-    for (int k = lane; k < a.ins; k += 64) {
-        const uint8_t c = a.w[((int64_t)n * a.blocks + (k >> 5)) * 16 + ((k & 31) >> 1)];
-        sum += seq_to_f32(x[k]) * (matvec_code(k & 1 ? c >> 4 : c & 15) * matvec_scale(a.w_scale[(int64_t)n * a.blocks + (k >> 5)]));
+    typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf16x2;
+    const float f = __uint_as_float(scale << 23);
+    union { bf16x2 two[4]; bf16x8 all; } r;
+    r.two[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, f, 0);
+    r.two[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, f, 1);
+    r.two[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, f, 2);
+    r.two[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, f, 3);
+    return r.all;
+}
+// the same by 2^-8, which keeps every code of every scale finite; a scale of 255 is not a number
+__device__ __forceinline__ bf16x8 matvec_wide_slow(uint32_t c, uint32_t scale)
+{
+    union { uint32_t w[4]; bf16x8 all; } r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float v[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const uint32_t code = c >> (8 * i + 4 * h) & 15, m = code & 7;
+            float f = m < 2 ? 0.5f * (float)m : __uint_as_float((126 + (m >> 1)) << 23 | (m & 1) << 22);
+            f *= scale == 255 ? __builtin_nanf("") : scale > 8 ? __uint_as_float((scale - 8) << 23) : 0.f;
+            v[h] = code & 8 ? -f : f;
+        }
+        r.w[i] = seq_pack_bf16(v[0], v[1]);
     }
-    for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
-    if (lane) return;
-    if (a.x_scale) sum *= a.x_scale[m];
-    if (a.relu) sum = sum < 0.f ? 0.f : sum;
-    ((Y*)a.y)[m * a.y_stride + n] = (Y)sum;
+    return r.all;
 }
 
-template <typename T>
-static void launch_matvec(hipStream_t s, const matvec_args& a, int y_type)
+template <int XT, int MT, int R>
+__global__ __launch_bounds__(64 * MATVEC_WAVES) void k_seq_matvec(matvec_args a)
 {
-    const dim3 grid((a.outs + 3) / 4, a.rows);
-    if (y_type == RH_T_F32) hipLaunchKernelGGL((k_seq_matvec<T, float>), grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((k_seq_matvec<T, __bf16>), grid, dim3(256), 0, s, a);
+    typedef matvec_kind<XT> K;
+    typedef typename K::T T;
+    constexpr int PARTS = K::PARTS, PIECE = K::PIECE, PER_STEP = 128 / PIECE;      // 16-byte pieces of a row in a step of 128
+    extern __shared__ uint4 s_mem[];
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6, c = lane & 15, j = lane >> 4;
+    const int tw = wave / a.ks, ks = wave % a.ks;
+    const int m0 = blockIdx.y * 16 * MT, M = a.rows - m0 < 16 * MT ? a.rows - m0 : 16 * MT;
+    // x in LDS: pieces of 16 bytes, [part][step][as the lanes of a product read them][row]
+    const int part_pieces = a.chunk * 4 * PER_STEP * M;
+    u32x4* xs = (u32x4*)s_mem;
+    f32x4* s_sum = (f32x4*)(xs + PARTS * part_pieces);       // [wave][R * MT][lane]
+
+    auto stage = [&](int q0, int nq) {
+        const int per_row = nq * 4 * PER_STEP;               // pieces of a row
+        for (int i = t; i < per_row * M; i += blockDim.x) {
+            const int m = i / per_row, p = i - m * per_row;  // piece p: elements k .. k + PIECE of row m
+            const int k = q0 * 512 + p * PIECE, n = a.ins - k;
+            const T* from = (const T*)a.x + (m0 + m) * a.x_stride + k;
+            // bf16: lane quarter j of the e-th product of a step reads block j's piece e; the scaled product has pieces j and 4 + j there
+            const int step = p / PER_STEP, in = p % PER_STEP;
+            u32x4* to = xs + (step * PER_STEP + (XT == MATVEC_SCALED ? in : in % 4 * 4 + in / 4)) * M + m;
+            if constexpr (XT == RH_T_F32) {
+                uint32_t w[3][4];
+#pragma unroll
+                for (int d = 0; d < 8; d += 2) {
+                    uint32_t lo[3], hi[3];
+                    matvec_cut(d < n ? from[d] : 0.f, lo);
+                    matvec_cut(d + 1 < n ? from[d + 1] : 0.f, hi);
+#pragma unroll
+                    for (int s = 0; s < 3; ++s) w[s][d / 2] = lo[s] | hi[s] << 16;
+                }
+#pragma unroll
+                for (int s = 0; s < 3; ++s) to[s * part_pieces] = u32x4{w[s][0], w[s][1], w[s][2], w[s][3]};
+            } else {
+                constexpr int W = PIECE * sizeof(T) / 4;     // words of x
+                uint32_t v[W] = {};
+                if (n >= PIECE) {
+                    if constexpr (W == 4) { const u32x4 u = seq_load<u32x4>(from); v[0] = u[0]; v[1] = u[1]; v[2] = u[2]; v[3] = u[3]; }
+                    else { const uint2 u = seq_load<uint2>(from); v[0] = u.x; v[1] = u.y; }
+                } else if (n > 0) {
+#pragma unroll
+                    for (int d = 0; d < PIECE; ++d) {
+                        const uint32_t bits = d < n ? (sizeof(T) == 2 ? *(const uint16_t*)(from + d) : *(const uint8_t*)(from + d)) : 0;
+                        v[d * sizeof(T) / 4] |= bits << (8 * sizeof(T) * (d % (4 / sizeof(T))));
+                    }
+                }
+                if constexpr (W == 4) *to = u32x4{v[0], v[1], v[2], v[3]};
+                else *to = u32x4{seq_e4m3_pair<false>(v[0]), seq_e4m3_pair<true>(v[0]), seq_e4m3_pair<false>(v[1]), seq_e4m3_pair<true>(v[1])};
+            }
+        }
+    };
+
+    // ---- a wave's weights: tile by tile of outputs, of each its share of the stretches of every chunk
+    struct place { int tile, q0, q, end; };                  // q0: the chunk's first stretch; q, end: of the wave's share, in the chunk
+    auto share = [&](place& p) {
+        const int n = a.quads - p.q0 < a.chunk ? a.quads - p.q0 : a.chunk, each = (n + a.ks - 1) / a.ks;
+        p.q = ks * each;
+        p.end = p.q + each < n ? p.q + each : n;
+    };
+    const int tile_step = gridDim.x * a.tw;
+    // the next stretch, of this chunk or of a later chunk or tile; false: there is none
+    auto advance = [&](place& p) -> bool {
+        ++p.q;
+        while (p.q >= p.end) {
+            p.q0 += a.chunk;
+            if (p.q0 >= a.quads) { p.q0 = 0; p.tile += tile_step; }
+            if (p.tile >= a.tiles) return false;
+            share(p);
+        }
+        return true;
+    };
+    struct weights { u32x4 code[R][4]; u32x4 scale[R]; };
+    auto load = [&](const place& p, weights& w) {
+        const int quad = p.q0 + p.q;
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            int n = (p.tile * R + r) * 16 + c;
+            n = n < a.outs ? n : a.outs - 1;
+            const int b0 = quad * 16;                        // the stretch's first block
+            const uint8_t* code = a.w + ((int64_t)n * a.blocks + b0) * 16;
+            const uint8_t* scale = a.w_scale + (int64_t)n * a.blocks + b0;
+            if (b0 + 16 <= a.blocks) {
+#pragma unroll
+                for (int s = 0; s < 4; ++s) w.code[r][s] = *(const u32x4*)(code + (4 * s + j) * 16);
+                w.scale[r] = seq_load<u32x4>(scale);
+            } else {
+#pragma unroll
+                for (int s = 0; s < 4; ++s) {
+                    const bool in = b0 + 4 * s + j < a.blocks;   // a block that is none: codes of zero, a scale of one
+                    const u32x4 v = *(const u32x4*)(in ? code + (4 * s + j) * 16 : a.w);
+                    w.code[r][s] = in ? v : u32x4{0, 0, 0, 0};
+                    uint32_t e = 0;
+#pragma unroll
+                    for (int b = 0; b < 4; ++b) e |= (uint32_t)(b0 + 4 * s + b < a.blocks ? scale[4 * s + b] : 127) << (8 * b);
+                    w.scale[r][s] = e;
+                }
+            }
+        }
+    };
+
+    f32x4 acc[R][MT];
+    int mrow[MT];                                            // rows that are none read row 0
+#pragma unroll
+    for (int i = 0; i < MT; ++i) mrow[i] = j * M + (16 * i + c < M ? 16 * i + c : 0);
+
+    auto multiply = [&](const weights& w, int q) {
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            const u32x4* x = xs + (q * 4 + s) * PER_STEP * M;
+            if constexpr (XT == MATVEC_SCALED) {
+                i32x8 xb[MT];
+#pragma unroll
+                for (int i = 0; i < MT; ++i) {
+                    const u32x4 lo = x[mrow[i]], hi = x[4 * M + mrow[i]];
+                    xb[i] = i32x8{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+                }
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    const u32x4 u = w.code[r][s];
+                    const i32x8 wa = {(int)u[0], (int)u[1], (int)u[2], (int)u[3], 0, 0, 0, 0};
+                    const int scale = (int)(w.scale[r][s] >> (8 * j));
+#pragma unroll
+                    for (int i = 0; i < MT; ++i)
+                        acc[r][i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wa, xb[i], acc[r][i], 4, 0, 0, scale, 0, 127);
+                }
+            } else {
+                uint32_t scale[R];
+                bool huge = false;
+#pragma unroll
+                for (int r = 0; r < R; ++r) { scale[r] = w.scale[r][s] >> (8 * j) & 255; huge |= scale[r] >= MATVEC_HUGE; }
+                if (!__any(huge)) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        bf16x8 wa[R];
+#pragma unroll
+                        for (int r = 0; r < R; ++r) wa[r] = matvec_wide(w.code[r][s][e], scale[r]);
+#pragma unroll
+                        for (int p = PARTS - 1; p >= 0; --p)
+#pragma unroll
+                            for (int i = 0; i < MT; ++i) {
+                                const bf16x8 xb = __builtin_bit_cast(bf16x8, x[p * part_pieces + e * 4 * M + mrow[i]]);
+#pragma unroll
+                                for (int r = 0; r < R; ++r) acc[r][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wa[r], xb, acc[r][i], 0, 0, 0);
+                            }
+                    }
+                } else {
+                    // codes that bf16 cannot hold: this step's products by 2^-8, on their own
+                    f32x4 part[R][MT];
+#pragma unroll
+                    for (int r = 0; r < R; ++r)
+#pragma unroll
+                        for (int i = 0; i < MT; ++i) part[r][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+                    for (int e = 0; e < 4; ++e)
+#pragma unroll
+                        for (int r = 0; r < R; ++r) {
+                            const uint32_t code = e == 0 ? w.code[r][s][0] : e == 1 ? w.code[r][s][1] : e == 2 ? w.code[r][s][2] : w.code[r][s][3];
+                            const bf16x8 wa = matvec_wide_slow(code, scale[r]);
+#pragma unroll
+                            for (int p = PARTS - 1; p >= 0; --p)
+#pragma unroll
+                                for (int i = 0; i < MT; ++i)
+                                    part[r][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wa, __builtin_bit_cast(bf16x8, x[p * part_pieces + e * 4 * M + mrow[i]]), part[r][i], 0, 0, 0);
+                        }
+#pragma unroll
+                    for (int r = 0; r < R; ++r)
+#pragma unroll
+                        for (int i = 0; i < MT; ++i) acc[r][i] += part[r][i] * 256.f;
+                }
+            }
+        }
+    };
+
+    auto write = [&](int tile) {
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+                const int m = 16 * i + c, n = (tile * R + r) * 16 + 4 * j;
+                if (m >= M || n >= a.outs) continue;
+                f32x4 v = acc[r][i];
+                if (a.x_scale) v *= a.x_scale[m0 + m];
+                if (a.relu) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[e] = v[e] < 0.f ? 0.f : v[e];
+                }
+                const int64_t at = (m0 + m) * a.y_stride + n;
+                if (a.y_f32) {
+                    float* o = (float*)a.y + at;
+                    if (n + 4 <= a.outs) seq_store(o, v);
+                    else for (int e = 0; n + e < a.outs; ++e) o[e] = v[e];
+                } else {
+                    __bf16* o = (__bf16*)a.y + at;
+                    if (n + 4 <= a.outs) seq_store(o, make_uint2(seq_pack_bf16(v[0], v[1]), seq_pack_bf16(v[2], v[3])));
+                    else for (int e = 0; n + e < a.outs; ++e) o[e] = (__bf16)v[e];
+                }
+            }
+    };
+
+    place at = {(int)blockIdx.x * a.tw + tw, 0, 0, 0};
+    weights now, next;
+    bool have = at.tile < a.tiles;
+    if (have) {
+        share(at);
+        if (at.q >= at.end) { at.q = at.end; have = advance(at); }
+        if (have) load(at, now);
+    }
+    int staged = -1;                                         // the chunk that is in LDS
+    for (int first = blockIdx.x * a.tw; first < a.tiles; first += tile_step) {     // the same rounds for every wave
+        const int tile = first + tw;
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int i = 0; i < MT; ++i) acc[r][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int q0 = 0; q0 < a.quads; q0 += a.chunk) {
+            if (staged != q0) {
+                if (staged >= 0) __syncthreads();
+                stage(q0, a.quads - q0 < a.chunk ? a.quads - q0 : a.chunk);
+                __syncthreads();
+                staged = q0;
+            }
+            while (have && at.tile == tile && at.q0 == q0) {
+                const int q = at.q;
+                have = advance(at);
+                if (have) load(at, next);
+                multiply(now, q);
+                now = next;
+            }
+        }
+        if (a.ks > 1) {
+            __syncthreads();                                 // the sums of the round before have been read
+            if (ks) {
+#pragma unroll
+                for (int r = 0; r < R; ++r)
+#pragma unroll
+                    for (int i = 0; i < MT; ++i) s_sum[(wave * R * MT + r * MT + i) * 64 + lane] = acc[r][i];
+            }
+            __syncthreads();
+            if (!ks) {
+                for (int k = 1; k < a.ks; ++k)
+#pragma unroll
+                    for (int r = 0; r < R; ++r)
+#pragma unroll
+                        for (int i = 0; i < MT; ++i) acc[r][i] += s_sum[((wave + k) * R * MT + r * MT + i) * 64 + lane];
+            }
+        }
+        if (!ks && tile < a.tiles) write(tile);
+    }
+}
+
+template <int XT, int MT, int R>
+static hipError_t launch_matvec(rh_ctx* ctx, matvec_args a)
+{
+    typedef matvec_kind<XT> K;
+    static bool attr_done[RH_MAX_DEVICES] = {};              // the attribute is per device
+    if (!attr_done[ctx->device]) {
+        const hipError_t e = hipFuncSetAttribute((const void*)k_seq_matvec<XT, MT, R>, hipFuncAttributeMaxDynamicSharedMemorySize, MATVEC_LDS);
+        if (e != hipSuccess) return e;
+        attr_done[ctx->device] = true;
+    }
+    const int M = a.rows < 16 * MT ? a.rows : 16 * MT, quad = K::PARTS * 512 / K::PIECE * 16 * M;       // bytes of x in LDS, of a stretch
+    const int sums = MATVEC_WAVES * R * MT * 64 * (int)sizeof(f32x4);
+    a.quads = (a.ins + 511) / 512;
+    a.chunk = (MATVEC_LDS - sums) / quad;
+    a.chunk = a.chunk < a.quads ? a.chunk : a.quads;
+    a.tiles = (a.outs + 16 * R - 1) / (16 * R);
+    // Two workgroups a CU where their rows fit.  A tile a workgroup (several where there are more tiles than that), the other waves
+    // share its inner index.
+    const int wgs = ctx->n_cu * (a.chunk * quad + sums <= MATVEC_LDS / 2 ? 2 : 1);
+    const int each = (a.tiles + wgs - 1) / wgs;
+    a.tw = 1;
+    while (a.tw < each && a.tw < MATVEC_WAVES) a.tw *= 2;
+    a.ks = 1;
+    while (a.ks * a.tw < MATVEC_WAVES && a.ks < a.chunk) a.ks *= 2;
+    const int groups = (a.tiles + a.tw - 1) / a.tw;
+    hipLaunchKernelGGL((k_seq_matvec<XT, MT, R>), dim3(groups < wgs ? groups : wgs, (a.rows + 16 * MT - 1) / (16 * MT)), dim3(64 * a.tw * a.ks),
+                       (size_t)a.chunk * quad + (a.ks > 1 ? sums : 0), ctx->stream, a);
+    return hipGetLastError();
 }
 
 extern "C" rh_status rh_matvec_packed(rh_ctx* ctx, const void* x, int32_t x_type, int64_t x_stride, const float* x_scale,
@@ -62,10 +378,16 @@ extern "C" rh_status rh_matvec_packed(rh_ctx* ctx, const void* x, int32_t x_type
     if (x_stride < n_in || y_stride < n_out) RH_FAIL(ctx, RH_E_SHAPE, "rh_matvec_packed: a row stride below the row's length");
     if ((uintptr_t)w & 15) RH_FAIL(ctx, RH_E_INVALID, "rh_matvec_packed: w must be 16-byte aligned");
     if (n_rows == 0) return RH_OK;
-    const matvec_args a = {x, x_scale, w, w_scale, y, x_stride, y_stride, n_rows, n_out, n_in, (n_in + 31) / 32, relu};
-    if (x_type == RH_T_F32) launch_matvec<float>(ctx->stream, a, y_type);
-    else if (x_type == RH_T_BF16) launch_matvec<__bf16>(ctx->stream, a, y_type);
-    else launch_matvec<uint8_t>(ctx->stream, a, y_type);
-    RH_HIP(ctx, hipGetLastError());
+    matvec_args a = {};
+    a.x = x; a.x_scale = x_scale; a.w = w; a.w_scale = w_scale; a.y = y; a.x_stride = x_stride; a.y_stride = y_stride;
+    a.rows = n_rows; a.outs = n_out; a.ins = n_in; a.blocks = (n_in + 31) / 32; a.relu = relu; a.y_f32 = y_type == RH_T_F32;
+    // More rows a pass read the weights fewer times; what x takes of the LDS bounds them.
+    hipError_t e;
+    if (x_type == RH_T_F32) e = launch_matvec<RH_T_F32, 1, 1>(ctx, a);
+    else if (x_type == RH_T_BF16) e = n_rows <= 16 ? launch_matvec<RH_T_BF16, 1, 1>(ctx, a) : launch_matvec<RH_T_BF16, 2, 2>(ctx, a);
+    else if (y_type == RH_T_BF16 && n_in >= 512)
+        e = n_rows <= 16 ? launch_matvec<MATVEC_SCALED, 1, 1>(ctx, a) : n_rows <= 32 ? launch_matvec<MATVEC_SCALED, 2, 2>(ctx, a) : launch_matvec<MATVEC_SCALED, 4, 2>(ctx, a);
+    else e = n_rows <= 16 ? launch_matvec<RH_T_E4M3, 1, 1>(ctx, a) : launch_matvec<RH_T_E4M3, 2, 2>(ctx, a);
+    RH_HIP(ctx, e);
     return RH_OK;
 }
