@@ -24,6 +24,7 @@ struct matvec_args {
     int32_t tiles, ks, tw;       // tiles of outputs; waves a tile; tiles a workgroup at a time
     int32_t quads, chunk;        // stretches of 512 of the inner index: all, and as many as x lies in LDS for at a time
     int32_t y_f32;
+    seq_div row_pieces[2];       // 16-byte pieces of a row in LDS: of a whole chunk, of the last
 };
 
 #define MATVEC_WAVES 8
@@ -82,7 +83,7 @@ __device__ __forceinline__ bf16x8 matvec_wide_slow(uint32_t c, uint32_t scale)
 }
 
 template <int XT, int MT, int R>
-__global__ __launch_bounds__(64 * MATVEC_WAVES) void k_seq_matvec(matvec_args a)
+__global__ __launch_bounds__(64 * MATVEC_WAVES, MT == 1 ? 4 : 2) void k_seq_matvec(matvec_args a)
 {
     typedef matvec_kind<XT> K;
     typedef typename K::T T;
@@ -96,44 +97,68 @@ __global__ __launch_bounds__(64 * MATVEC_WAVES) void k_seq_matvec(matvec_args a)
     u32x4* xs = (u32x4*)s_mem;
     f32x4* s_sum = (f32x4*)(xs + PARTS * part_pieces);       // [wave][R * MT][lane]
 
+    constexpr int W = PIECE * sizeof(T) / 4;                 // words of a piece in memory
+    auto put = [&](int m, int p, const uint32_t* v) {        // piece p of row m
+        // bf16: lane quarter j of the e-th product of a step reads block j's piece e; the scaled product has pieces j and 4 + j there
+        const int step = p / PER_STEP, in = p % PER_STEP;
+        u32x4* to = xs + (step * PER_STEP + (XT == MATVEC_SCALED ? in : in % 4 * 4 + in / 4)) * M + m;
+        if constexpr (XT == RH_T_F32) {
+            uint32_t w[3][4];
+#pragma unroll
+            for (int d = 0; d < 8; d += 2) {
+                uint32_t lo[3], hi[3];
+                matvec_cut(__uint_as_float(v[d]), lo);
+                matvec_cut(__uint_as_float(v[d + 1]), hi);
+#pragma unroll
+                for (int s = 0; s < 3; ++s) w[s][d / 2] = lo[s] | hi[s] << 16;
+            }
+#pragma unroll
+            for (int s = 0; s < 3; ++s) to[s * part_pieces] = u32x4{w[s][0], w[s][1], w[s][2], w[s][3]};
+        } else if constexpr (W == 4) *to = u32x4{v[0], v[1], v[2], v[3]};
+        else *to = u32x4{seq_e4m3_pair<false>(v[0]), seq_e4m3_pair<true>(v[0]), seq_e4m3_pair<false>(v[1]), seq_e4m3_pair<true>(v[1])};
+    };
+    auto get = [&](const T* from, uint32_t* v) {             // a whole piece
+        if constexpr (W == 2) { const uint2 u = seq_load<uint2>(from); v[0] = u.x; v[1] = u.y; }
+        else
+#pragma unroll
+            for (int d = 0; d < W; d += 4) {
+                const u32x4 u = seq_load<u32x4>((const uint32_t*)from + d);
+                v[d] = u[0]; v[d + 1] = u[1]; v[d + 2] = u[2]; v[d + 3] = u[3];
+            }
+    };
     auto stage = [&](int q0, int nq) {
-        const int per_row = nq * 4 * PER_STEP;               // pieces of a row
-        for (int i = t; i < per_row * M; i += blockDim.x) {
-            const int m = i / per_row, p = i - m * per_row;  // piece p: elements k .. k + PIECE of row m
-            const int k = q0 * 512 + p * PIECE, n = a.ins - k;
-            const T* from = (const T*)a.x + (m0 + m) * a.x_stride + k;
-            // bf16: lane quarter j of the e-th product of a step reads block j's piece e; the scaled product has pieces j and 4 + j there
-            const int step = p / PER_STEP, in = p % PER_STEP;
-            u32x4* to = xs + (step * PER_STEP + (XT == MATVEC_SCALED ? in : in % 4 * 4 + in / 4)) * M + m;
-            if constexpr (XT == RH_T_F32) {
-                uint32_t w[3][4];
+        const int per_row = nq * 4 * PER_STEP, all = per_row * M;                          // pieces: of a row, of all
+        const seq_div& div = a.row_pieces[nq < a.chunk];
+        if ((q0 + nq) * 512 <= a.ins) {
+            constexpr int AHEAD = 4;                         // pieces of a thread in flight
+            for (int first = t; first < all; first += AHEAD * blockDim.x) {
+                uint32_t v[AHEAD][W];
+                int m[AHEAD], p[AHEAD];
 #pragma unroll
-                for (int d = 0; d < 8; d += 2) {
-                    uint32_t lo[3], hi[3];
-                    matvec_cut(d < n ? from[d] : 0.f, lo);
-                    matvec_cut(d + 1 < n ? from[d + 1] : 0.f, hi);
-#pragma unroll
-                    for (int s = 0; s < 3; ++s) w[s][d / 2] = lo[s] | hi[s] << 16;
+                for (int k = 0; k < AHEAD; ++k) {            // behind the last: the last again
+                    int i = first + k * (int)blockDim.x;
+                    i = i < all ? i : all - 1;
+                    m[k] = (int)seq_quot((uint32_t)i, div); p[k] = i - m[k] * per_row;
+                    get((const T*)a.x + (m0 + m[k]) * a.x_stride + q0 * 512 + p[k] * PIECE, v[k]);
                 }
 #pragma unroll
-                for (int s = 0; s < 3; ++s) to[s * part_pieces] = u32x4{w[s][0], w[s][1], w[s][2], w[s][3]};
-            } else {
-                constexpr int W = PIECE * sizeof(T) / 4;     // words of x
+                for (int k = 0; k < AHEAD; ++k) put(m[k], p[k], v[k]);
+            }
+        } else
+            for (int i = t; i < all; i += blockDim.x) {      // rows that end in here: zeros behind
+                const int m = (int)seq_quot((uint32_t)i, div), p = i - m * per_row, e = q0 * 512 + p * PIECE, n = a.ins - e;
+                const T* from = (const T*)a.x + (m0 + m) * a.x_stride + e;
                 uint32_t v[W] = {};
-                if (n >= PIECE) {
-                    if constexpr (W == 4) { const u32x4 u = seq_load<u32x4>(from); v[0] = u[0]; v[1] = u[1]; v[2] = u[2]; v[3] = u[3]; }
-                    else { const uint2 u = seq_load<uint2>(from); v[0] = u.x; v[1] = u.y; }
-                } else if (n > 0) {
+                if (n >= PIECE) get(from, v);
+                else if (n > 0) {
 #pragma unroll
                     for (int d = 0; d < PIECE; ++d) {
-                        const uint32_t bits = d < n ? (sizeof(T) == 2 ? *(const uint16_t*)(from + d) : *(const uint8_t*)(from + d)) : 0;
+                        const uint32_t bits = d >= n ? 0 : sizeof(T) == 4 ? *(const uint32_t*)(from + d) : sizeof(T) == 2 ? *(const uint16_t*)(from + d) : *(const uint8_t*)(from + d);
                         v[d * sizeof(T) / 4] |= bits << (8 * sizeof(T) * (d % (4 / sizeof(T))));
                     }
                 }
-                if constexpr (W == 4) *to = u32x4{v[0], v[1], v[2], v[3]};
-                else *to = u32x4{seq_e4m3_pair<false>(v[0]), seq_e4m3_pair<true>(v[0]), seq_e4m3_pair<false>(v[1]), seq_e4m3_pair<true>(v[1])};
+                put(m, p, v);
             }
-        }
     };
 
     // ---- a wave's weights: tile by tile of outputs, of each its share of the stretches of every chunk
@@ -350,6 +375,8 @@ static hipError_t launch_matvec(rh_ctx* ctx, matvec_args a)
     a.chunk = (MATVEC_LDS - sums) / quad;
     a.chunk = a.chunk < a.quads ? a.chunk : a.quads;
     a.tiles = (a.outs + 16 * R - 1) / (16 * R);
+    a.row_pieces[0] = seq_make_div(a.chunk * (512 / K::PIECE));
+    a.row_pieces[1] = seq_make_div(a.quads % a.chunk ? a.quads % a.chunk * (512 / K::PIECE) : 1);
     // Two workgroups a CU where their rows fit.  A tile a workgroup (several where there are more tiles than that), the other waves
     // share its inner index.
     const int wgs = ctx->n_cu * (a.chunk * quad + sums <= MATVEC_LDS / 2 ? 2 : 1);
