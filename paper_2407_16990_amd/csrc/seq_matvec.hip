@@ -27,7 +27,7 @@ struct matvec_args {
     seq_div row_pieces[2];       // 16-byte pieces of a row in LDS: of a whole chunk, of the last
 };
 
-#define MATVEC_WAVES 8
+#define MATVEC_WAVES(XT, MT) (MT == 1 && XT != RH_T_F32 ? 16 : 8)       // of a workgroup, one a CU; the others' registers allow eight
 #define MATVEC_LDS (160 * 1024)
 #define MATVEC_HUGE 252          // scales from here on can take a code past the largest bf16 number
 
@@ -83,7 +83,7 @@ __device__ __forceinline__ bf16x8 matvec_wide_slow(uint32_t c, uint32_t scale)
 }
 
 template <int XT, int MT, int R>
-__global__ __launch_bounds__(64 * MATVEC_WAVES, MT == 1 ? 4 : 2) void k_seq_matvec(matvec_args a)
+__global__ __launch_bounds__(64 * MATVEC_WAVES(XT, MT)) void k_seq_matvec(matvec_args a)
 {
     typedef matvec_kind<XT> K;
     typedef typename K::T T;
@@ -370,21 +370,20 @@ static hipError_t launch_matvec(rh_ctx* ctx, matvec_args a)
         attr_done[ctx->device] = true;
     }
     const int M = a.rows < 16 * MT ? a.rows : 16 * MT, quad = K::PARTS * 512 / K::PIECE * 16 * M;       // bytes of x in LDS, of a stretch
-    const int sums = MATVEC_WAVES * R * MT * 64 * (int)sizeof(f32x4);
+    constexpr int WAVES = MATVEC_WAVES(XT, MT), sums = WAVES * R * MT * 64 * (int)sizeof(f32x4);
     a.quads = (a.ins + 511) / 512;
     a.chunk = (MATVEC_LDS - sums) / quad;
     a.chunk = a.chunk < a.quads ? a.chunk : a.quads;
     a.tiles = (a.outs + 16 * R - 1) / (16 * R);
     a.row_pieces[0] = seq_make_div(a.chunk * (512 / K::PIECE));
     a.row_pieces[1] = seq_make_div(a.quads % a.chunk ? a.quads % a.chunk * (512 / K::PIECE) : 1);
-    // Two workgroups a CU where their rows fit.  A tile a workgroup (several where there are more tiles than that), the other waves
-    // share its inner index.
-    const int wgs = ctx->n_cu * (a.chunk * quad + sums <= MATVEC_LDS / 2 ? 2 : 1);
-    const int each = (a.tiles + wgs - 1) / wgs;
+    // One workgroup a CU, so that x is laid out there once.  A tile a workgroup (several where there are more tiles than that), the other
+    // waves share its inner index.
+    const int wgs = ctx->n_cu, each = (a.tiles + wgs - 1) / wgs;
     a.tw = 1;
-    while (a.tw < each && a.tw < MATVEC_WAVES) a.tw *= 2;
+    while (a.tw < each && a.tw < WAVES) a.tw *= 2;
     a.ks = 1;
-    while (a.ks * a.tw < MATVEC_WAVES && a.ks < a.chunk) a.ks *= 2;
+    while (a.ks * a.tw < WAVES && a.ks < a.chunk) a.ks *= 2;
     const int groups = (a.tiles + a.tw - 1) / a.tw;
     hipLaunchKernelGGL((k_seq_matvec<XT, MT, R>), dim3(groups < wgs ? groups : wgs, (a.rows + 16 * MT - 1) / (16 * MT)), dim3(64 * a.tw * a.ks),
                        (size_t)a.chunk * quad + (a.ks > 1 ? sums : 0), ctx->stream, a);
