@@ -217,7 +217,7 @@ def _values(x, sc):
 
 def _check_attend(rh, q, cache, table, lengths, scale, window=0, got=None):
     out, lse = rh.cache_attend(q, cache, table, lengths, scale=scale, window=window, want_lse=True) if got is None else got
-    page = cache.desc.page
+    page = cache.page
     k, v = _values(cache.k, cache.k_scale), _values(cache.v, cache.v_scale)
     qn, t = _np(q), table.cpu().numpy()
     w_out, w_lse = S.attend(qn, k, v, t, lengths.cpu().numpy(), page, scale, window)
@@ -322,7 +322,7 @@ def test_attend_peaked_scores(rh, q_dtype, c_dtype):
 @pytest.mark.parametrize("q_dtype,c_dtype", KINDS)
 def test_attend_leaves_out_pages_that_do_not_exist(rh, q_dtype, c_dtype):
     q, cache, table, lengths = _attend_inputs(8, [100, 64, 31, 200], 2, 2, 64, 16, q_dtype, c_dtype, poison=False)
-    table[0, 2], table[1, :], table[2, 0], table[3, 5], table[3, 12] = -1, 10 ** 6, -5, cache.desc.n_pages, -(2 ** 31)
+    table[0, 2], table[1, :], table[2, 0], table[3, 5], table[3, 12] = -1, 10 ** 6, -5, cache.n_pages, -(2 ** 31)
     cache.v[0].view(torch.uint8)[:] = 0x7F                         # page 0 may hold anything where nobody owns it
     cache.k[0].view(torch.uint8)[:] = 0x7F
     table[table == 0] = -1
