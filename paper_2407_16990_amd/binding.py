@@ -241,6 +241,11 @@ class RH:
         if st != 0:
             raise RhError(st, self.lib.rh_last_error(self.h).decode())
 
+    def set_stream(self, stream) -> None:
+        """The torch stream that the calls go on from here."""
+        self._check(self.lib.rh_set_stream(self.h, C.c_void_p(stream.cuda_stream)))
+        self._stream = stream
+
     def budget(self, n_bins: int) -> int:
         return int(self.lib.rh_budget(self.cfg.bin_size, self.cfg.bin_size, n_bins))
 
