@@ -39,6 +39,7 @@ struct attend_args {
 #define ATTEND_CHUNK_MIN 4       // tiles
 #define ATTEND_CHUNK_FEW 32      // tiles a chunk up to which each CU gets one chunk
 #define ATTEND_CHUNKS 8          // chunks a CU beyond
+#define ATTEND_SOLO 8            // tiles of a stream that a wave takes alone, where there are many such streams and none longer
 #define ATTEND_FAN 16            // chunks joined at a time
 
 template <int KIND> struct attend_kind;
@@ -46,7 +47,6 @@ template <> struct attend_kind<RH_T_F32> { typedef float Q; typedef float C; sta
 template <> struct attend_kind<RH_T_BF16> { typedef __bf16 Q; typedef __bf16 C; static constexpr int TT = 2; };
 template <> struct attend_kind<RH_T_E4M3> { typedef __bf16 Q; typedef uint8_t C; static constexpr int TT = 2; };
 
-template <int N> struct attend_const { static constexpr int value = N; };
 template <int N> struct attend_words { uint32_t w[N]; };
 template <int N> __device__ __forceinline__ void attend_get(uint32_t* to, const void* from)
 {
@@ -55,8 +55,17 @@ template <int N> __device__ __forceinline__ void attend_get(uint32_t* to, const 
     else if constexpr (N == 2) { const uint2 u = *(const uint2*)from; to[0] = u.x; to[1] = u.y; }
     else { const uint4 u = *(const uint4*)from; to[0] = u.x; to[1] = u.y; to[2] = u.z; to[3] = u.w; }
 }
-template <int KIND, int D>
-__global__ __launch_bounds__(ATTEND_T) void k_seq_attend(attend_args a)
+// bytes of LDS for the keys and for the sums, whichever is more
+template <int KIND, int D> constexpr int attend_lds()
+{
+    constexpr int keys = ATTEND_WAVES * 16 * attend_kind<KIND>::TT * (D * (int)sizeof(typename attend_kind<KIND>::C) + 16);
+    constexpr int sums = ATTEND_WAVES / 2 * (D / 16 + 1) * 64 * (int)sizeof(f32x4);
+    return keys > sums ? keys : sums;
+}
+
+// MANY: more than 64 streams
+template <int KIND, int D, bool MANY>
+__global__ __launch_bounds__(ATTEND_T, D <= 128 ? 2 : 1) void k_seq_attend(attend_args a)
 {
     typedef typename attend_kind<KIND>::Q Q;
     typedef typename attend_kind<KIND>::C C;
@@ -71,54 +80,106 @@ __global__ __launch_bounds__(ATTEND_T) void k_seq_attend(attend_args a)
 
     extern __shared__ uint4 s_mem[];                         // the waves' keys; behind the loop, what half of the waves hand to the others
     f32x4(*s_acc)[NT + 1][64] = (f32x4(*)[NT + 1][64])s_mem;
+    __shared__ float s_some[ATTEND_WAVES];
+    __shared__ int32_t s_most[ATTEND_WAVES], s_sums[2][ATTEND_WAVES];
     __shared__ uint32_t s_last;
 
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6, c = lane & 15, j = lane >> 4;
     const int units = a.heads * a.head_tiles;
-    const int pair = (int)blockIdx.x / units, unit = (int)blockIdx.x % units;
 
-    // ---- which chunk: streams in order, each cut into chunks of `chunk` tiles
-    const int per = (a.n_streams + 63) / 64;
+    // ---- the streams' chunks: streams in order, each cut into chunks of `chunk` tiles.  Up to 64 streams every wave has one a lane;
+    // of more, a thread has `per` neighbours, and running sums go to LDS.
+    constexpr int PER = MANY ? RH_SEQ_MAX_STREAMS / ATTEND_T : 1;
+    const int per = MANY ? (a.n_streams + ATTEND_T - 1) / ATTEND_T : 1, b0 = MANY ? t * per : lane;
+    int32_t* s_first = (int32_t*)((uint8_t*)s_mem + attend_lds<KIND, D>());       // chunks before a stream, and of those before it the ones that need scratch memory
+    int32_t* s_row = s_first + RH_SEQ_MAX_STREAMS + 1;
     const int64_t row_cap = (int64_t)a.max_pages * a.page.d;
-    auto kept = [&](int b, int64_t& len) -> int64_t {
-        len = a.lengths[b];
-        len = len < 0 ? 0 : len > row_cap ? row_cap : len;
-        return a.window && len > a.window ? a.window : len;
+    auto clipped = [&](int b) -> int32_t { const int32_t n = a.lengths[b]; return n < 0 ? 0 : n > row_cap ? (int32_t)row_cap : n; };
+    auto tiles_of = [&](int32_t len) -> int32_t {
+        const uint32_t n = a.window && len > a.window ? a.window : len;
+        return (int32_t)((n + TILE - 1) / TILE);
     };
-    auto tiles = [&](int i) -> int32_t {                     // of stream lane * per + i
-        int64_t len;
-        return lane * per + i < a.n_streams ? (int32_t)((kept(lane * per + i, len) + TILE - 1) / TILE) : 0;
-    };
+    int32_t len[PER] = {}, most_tiles = 0;            // unused beyond `per`
     float some = 0.f;
-    for (int i = 0; i < per; ++i) some += (float)tiles(i);
 #pragma unroll
-    for (int o = 32; o; o >>= 1) some += __shfl_xor(some, o);
+    for (int i = 0; i < PER; ++i) {
+        if (i >= per) break;
+        len[i] = b0 + i < a.n_streams ? clipped(b0 + i) : 0;
+    }
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        if (i >= per) break;
+        const int32_t n = tiles_of(len[i]);
+        some += (float)n;
+        most_tiles = n > most_tiles ? n : most_tiles;
+    }
+    // Many short streams: a wave each, with nothing to join.  (128 streams of up to 256 tokens, 8 heads: 24.0 -> 19.5 us, of up to 64
+    // 16.7 -> 10.0.  Half as many streams gain up to fewer tiles: 64 of up to 30 tokens 7.1 -> 6.0, of up to 128 10.7 -> 12.2.)
+    const int few = a.n_streams * units / a.n_cu, cap = few < 4 ? few / 2 : ATTEND_SOLO;
+    bool longer = __any(most_tiles > cap);
+    some = seq_sum(some);
+    if constexpr (MANY) {
+        if (lane == 0) { s_some[wave] = some; s_most[wave] = longer; }
+        __syncthreads();
+        some = 0.f; longer = false;
+#pragma unroll
+        for (int w = 0; w < ATTEND_WAVES; ++w) { some += s_some[w]; longer |= s_most[w] != 0; }
+    }
+    const bool solo = !longer;
     const float all = some * (float)units, cus = (float)a.n_cu;
     int chunk = (int)ceilf(fmaxf(fminf(all / cus, (float)ATTEND_CHUNK_FEW), all / (cus * ATTEND_CHUNKS) * 1.0001f));
-    chunk = ((chunk < ATTEND_CHUNK_MIN ? ATTEND_CHUNK_MIN : chunk) + ATTEND_WAVES - 1) / ATTEND_WAVES * ATTEND_WAVES;
+    chunk = solo ? ATTEND_SOLO : ((chunk < ATTEND_CHUNK_MIN ? ATTEND_CHUNK_MIN : chunk) + ATTEND_WAVES - 1) / ATTEND_WAVES * ATTEND_WAVES;
     // a stream without tokens has one chunk, which writes its zeros; only chunks of streams that have several need scratch memory
-    auto chunks = [&](int i) -> int {
-        const int n = tiles(i);
-        return lane * per + i < a.n_streams ? n > chunk ? (n + chunk - 1) / chunk : 1 : 0;
-    };
-    int32_t mine = 0, shared = 0;
-    for (int i = 0; i < per; ++i) { const int n = chunks(i); mine += n; shared += n > 1 ? n : 0; }
-    int32_t before = seq_scan(mine) - mine, ahead = seq_scan(shared) - shared;
-    const uint64_t owner = __ballot(pair >= before && pair < before + mine);
-    if (!owner) return;                                      // the grid is as large as any lengths need
-    int32_t item[4] = {};
-    for (int i = 0; i < per; ++i) {
-        const int n = chunks(i);
-        if (pair >= before && pair < before + n) { item[0] = lane * per + i; item[1] = pair - before; item[2] = n; item[3] = ahead; }
-        before += n; ahead += n > 1 ? n : 0;
+    int32_t n_chunks[PER], mine = 0, shared = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        if (i >= per) break;
+        const int32_t n = tiles_of(len[i]);
+        n_chunks[i] = b0 + i >= a.n_streams ? 0 : 1;
+        if (n > chunk) n_chunks[i] = (n + chunk - 1) / chunk;
+        mine += n_chunks[i];
+        shared += n_chunks[i] > 1 ? n_chunks[i] : 0;
     }
-    const int who = __builtin_ctzll(owner);
-    const int b = __builtin_amdgcn_readlane(item[0], who), split = __builtin_amdgcn_readlane(item[1], who);
-    const int n_split = __builtin_amdgcn_readlane(item[2], who), first_row = __builtin_amdgcn_readlane(item[3], who);
-    int64_t len64;
-    const int64_t n_kept = kept(b, len64);
-    const int32_t len = (int32_t)len64, begin = (int32_t)(len64 - n_kept);
-    const int32_t n_tiles = (int32_t)((n_kept + TILE - 1) / TILE);
+    int32_t before = seq_scan(mine), ahead = seq_scan(shared), pairs = __builtin_amdgcn_readlane(before, 63);
+    before -= mine; ahead -= shared;
+    if constexpr (MANY) {
+        if (lane == 63) { s_sums[0][wave] = before + mine; s_sums[1][wave] = ahead + shared; }
+        __syncthreads();
+        pairs = 0;
+#pragma unroll
+        for (int w = 0; w < ATTEND_WAVES; ++w) {
+            if (w < wave) { before += s_sums[0][w]; ahead += s_sums[1][w]; }
+            pairs += s_sums[0][w];
+        }
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            if (i >= per) break;
+            if (b0 + i < a.n_streams) { s_first[b0 + i] = before; s_row[b0 + i] = ahead; }
+            before += n_chunks[i]; ahead += n_chunks[i] > 1 ? n_chunks[i] : 0;
+        }
+        if (t == 0) s_first[a.n_streams] = pairs;
+        __syncthreads();
+    }
+
+    // ---- this wave's chunk
+    const int64_t index = solo ? (int64_t)blockIdx.x * ATTEND_WAVES + wave : (int64_t)blockIdx.x;
+    if (index >= (int64_t)pairs * units) return;             // the grid is as large as any lengths need; a workgroup's waves part only where they go alone
+    const int pair = (int)((uint32_t)index / (uint32_t)units), unit = (int)((uint32_t)index % (uint32_t)units);
+    int b = 0, length, split, n_split, first_row;
+    if constexpr (MANY) {
+        for (int hi = a.n_streams; hi - b > 1;) { const int mid = (b + hi) >> 1; if (s_first[mid] <= pair) b = mid; else hi = mid; }
+        b = __builtin_amdgcn_readfirstlane(b);
+        const int first = __builtin_amdgcn_readfirstlane(s_first[b]);
+        split = pair - first; n_split = __builtin_amdgcn_readfirstlane(s_first[b + 1]) - first;
+        first_row = __builtin_amdgcn_readfirstlane(s_row[b]);
+        length = clipped(b);
+    } else {
+        b = __builtin_ctzll(__ballot(pair >= before && pair < before + mine));
+        length = __builtin_amdgcn_readlane(len[0], b); split = pair - __builtin_amdgcn_readlane(before, b);
+        n_split = __builtin_amdgcn_readlane(mine, b); first_row = __builtin_amdgcn_readlane(ahead, b);
+    }
+    const int32_t n_kept = a.window && length > a.window ? a.window : length, begin = length - n_kept;
+    const int32_t n_tiles = (int32_t)(((int64_t)n_kept + TILE - 1) / TILE);
     const int32_t tile_end = n_tiles < (split + 1) * chunk ? n_tiles : (split + 1) * chunk;
 
     const int kvh = unit / a.head_tiles, h0 = kvh * a.group + unit % a.head_tiles * 16;
@@ -145,7 +206,7 @@ __global__ __launch_bounds__(ATTEND_T) void k_seq_attend(attend_args a)
     const int32_t* table = a.table + (int64_t)b * a.max_pages;
     auto entry = [&](int32_t tile) -> int32_t {              // the table's word for this lane's token, -1 behind the last
         const uint32_t pos = (uint32_t)begin + (uint32_t)tile * TILE + (lane & (TILE - 1));
-        const bool in = tile < tile_end && pos < (uint32_t)len;
+        const bool in = tile < tile_end && pos < (uint32_t)length;
         const int32_t p = table[in ? seq_quot(pos, a.page) : 0];         // no branch around the load: the loads in flight stay countable
         return in ? p : -1;
     };
@@ -207,13 +268,14 @@ __global__ __launch_bounds__(ATTEND_T) void k_seq_attend(attend_args a)
     for (int i = 0; i < NT; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
     float top = -INFINITY, total = 0.f;
 
-    int32_t tile = split * chunk + wave;
+    const int turn = solo ? 1 : ATTEND_WAVES;                // tiles from one of a wave's to its next
+    int32_t tile = split * chunk + (solo ? 0 : wave);
     if (tile < tile_end) {
         where now = place(tile, entry(tile));
         load_k(now);
         load_v(now);
-        int32_t next_entry = entry(tile + ATTEND_WAVES);
-        for (; tile < tile_end; tile += ATTEND_WAVES) {
+        int32_t next_entry = entry(tile + turn);
+        for (; tile < tile_end; tile += turn) {
             // scores: rows 4*j + i of token tile tt, head c
             stage_k();
             f32x4 sc[TT];
@@ -247,9 +309,9 @@ __global__ __launch_bounds__(ATTEND_T) void k_seq_attend(attend_args a)
                 }
             }
             // the next tile's keys, into the registers that the products have read (behind the last tile: page 0's first line, unused)
-            const where next = place(tile + ATTEND_WAVES, next_entry);
+            const where next = place(tile + turn, next_entry);
             load_k(next);
-            const int32_t after = entry(tile + 2 * ATTEND_WAVES);
+            const int32_t after = entry(tile + 2 * turn);
 
             // softmax over this tile: token 16*tt + 4*j + i is lane (16*tt + 4*j + i)'s
             float p[ROWS], vs[ROWS], most = -INFINITY;
@@ -390,9 +452,11 @@ __global__ __launch_bounds__(ATTEND_T) void k_seq_attend(attend_args a)
         }
     };
 
-    __syncthreads();                                         // no wave needs its keys any more
-    join_waves();
-    if (wave == 0) {
+    if (!solo) {
+        __syncthreads();                                     // no wave needs its keys any more
+        join_waves();
+    }
+    if (wave == 0 || solo) {
         total += __shfl_xor(total, 16);
         total += __shfl_xor(total, 32);
     }
@@ -464,7 +528,7 @@ __global__ __launch_bounds__(ATTEND_T) void k_seq_attend(attend_args a)
                     if (quarter < 4) s_acc[0][NT][quarter * 16 + h] = f32x4{m, tot, 0.f, 0.f};
                 }
             };
-            if (n <= 4) join_rows(attend_const<4>()); else join_rows(attend_const<ATTEND_FAN>());
+            if (n <= 4) join_rows(seq_const<4>()); else join_rows(seq_const<ATTEND_FAN>());
             __syncthreads();
             if (wave == 0) {
 #pragma unroll
@@ -475,21 +539,22 @@ __global__ __launch_bounds__(ATTEND_T) void k_seq_attend(attend_args a)
         }
         at /= ATTEND_FAN; members = (members + ATTEND_FAN - 1) / ATTEND_FAN; stride *= ATTEND_FAN;
     }
-    if (wave == 0) write();
+    if (wave == 0 || solo) write();
 }
 
 template <int KIND, int D>
 static hipError_t launch_attend(rh_ctx* ctx, const attend_args& a, int64_t grid)
 {
-    constexpr int row = D * sizeof(typename attend_kind<KIND>::C) + 16, keys = ATTEND_WAVES * 16 * attend_kind<KIND>::TT * row;
-    constexpr int sums = ATTEND_WAVES / 2 * (D / 16 + 1) * 64 * (int)sizeof(f32x4), lds = keys > sums ? keys : sums;
+    constexpr int lds = attend_lds<KIND, D>(), sums = (2 * RH_SEQ_MAX_STREAMS + 1) * (int)sizeof(int32_t);
     static bool attr_done[RH_MAX_DEVICES] = {};              // the attribute is per device
     if (!attr_done[ctx->device]) {
-        const hipError_t e = hipFuncSetAttribute((const void*)k_seq_attend<KIND, D>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+        hipError_t e = hipFuncSetAttribute((const void*)k_seq_attend<KIND, D, false>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+        if (e == hipSuccess) e = hipFuncSetAttribute((const void*)k_seq_attend<KIND, D, true>, hipFuncAttributeMaxDynamicSharedMemorySize, lds + sums);
         if (e != hipSuccess) return e;
         attr_done[ctx->device] = true;
     }
-    hipLaunchKernelGGL((k_seq_attend<KIND, D>), dim3((unsigned)grid), dim3(ATTEND_T), lds, ctx->stream, a);
+    if (a.n_streams > 64) hipLaunchKernelGGL((k_seq_attend<KIND, D, true>), dim3((unsigned)grid), dim3(ATTEND_T), lds + sums, ctx->stream, a);
+    else hipLaunchKernelGGL((k_seq_attend<KIND, D, false>), dim3((unsigned)grid), dim3(ATTEND_T), lds, ctx->stream, a);
     return hipGetLastError();
 }
 
@@ -536,12 +601,12 @@ extern "C" rh_status rh_cache_attend(rh_ctx* ctx, const rh_kv_cache* cache, cons
     a.head_tiles = (a.group + 15) / 16; a.max_pages = max_pages; a.n_streams = n_streams; a.window = window; a.n_cu = ctx->n_cu;
     a.scale = scale * 1.44269504089f;
     // Chunks: at most ATTEND_CHUNKS a CU and one more for every stream and unit; less where the table's rows are short.
-    const int64_t units = (int64_t)cache->heads * a.head_tiles, streams_units = units * n_streams;
+    const int64_t streams_units = (int64_t)cache->heads * a.head_tiles * n_streams;
     const int64_t longest = window && window < (int64_t)max_pages * cache->page ? window : (int64_t)max_pages * cache->page;
     const int tile = cache->type == RH_T_F32 ? 16 : 32;
-    const int64_t most = (int64_t)ATTEND_CHUNKS * ctx->n_cu + streams_units;
     const int64_t cut = (longest + tile * ATTEND_CHUNK_MIN - 1) / (tile * ATTEND_CHUNK_MIN);
-    const int64_t grid = streams_units * cut < most ? streams_units * cut : most;
+    int64_t grid = (int64_t)ATTEND_CHUNKS * ctx->n_cu + streams_units;
+    grid = streams_units * cut < grid ? streams_units * cut : grid;
     // a stream cut into n > 1 chunks has more than n - 1 >= n / 2 chunks' tiles: at most twice ATTEND_CHUNKS a CU of them need scratch memory
     const size_t rows = (size_t)2 * ATTEND_CHUNKS * ctx->n_cu;
     const rh_status ws = seq_ensure(ctx, rows * (cache->dim / 16 * 64 + 16) * 16, rows);

@@ -34,6 +34,8 @@ __device__ __forceinline__ uint32_t seq_pack_e4m3(float a, float b, float c, flo
     return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, r, true);
 }
 
+template <int N> struct seq_const { static constexpr int value = N; };
+
 // Inclusive running sum over the wave's lanes, by row shifts and row broadcasts of the vector ALU.
 __device__ __forceinline__ int32_t seq_scan(int32_t v)
 {
@@ -44,6 +46,20 @@ __device__ __forceinline__ int32_t seq_scan(int32_t v)
     v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);        // the last lane of rows 0 and 2 to rows 1 and 3
     v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);        // lane 31 to the upper half
     return v;
+}
+
+__device__ __forceinline__ float seq_sum(float v)            // of the wave, the same for every lane
+{
+    auto from = [](float x, auto ctrl, auto rows) {
+        return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), decltype(ctrl)::value, decltype(rows)::value, 0xF, decltype(rows)::value == 0xF));
+    };
+    v += from(v, seq_const<0x111>(), seq_const<0xF>());
+    v += from(v, seq_const<0x112>(), seq_const<0xF>());
+    v += from(v, seq_const<0x114>(), seq_const<0xF>());
+    v += from(v, seq_const<0x118>(), seq_const<0xF>());
+    v += from(v, seq_const<0x142>(), seq_const<0xA>());
+    v += from(v, seq_const<0x143>(), seq_const<0xC>());
+    return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v), 63));
 }
 
 // A vector in memory that need not be aligned: global loads and stores take any byte address, and one instruction
