@@ -30,7 +30,7 @@ struct attend_args {
     float *lse, *ws;
     uint32_t* count;
     seq_div page;
-    int32_t n_pages, heads, q_heads, group, head_tiles, max_pages, n_streams, window, n_cu;
+    int32_t n_pages, heads, q_heads, group, head_tiles, max_pages, n_streams, window, n_cu, grouped;
     float scale;             // times log2(e): the softmax runs on powers of two
 };
 
@@ -40,6 +40,7 @@ struct attend_args {
 #define ATTEND_CHUNK_FEW 32      // tiles a chunk up to which each CU gets one chunk
 #define ATTEND_CHUNKS 8          // chunks a CU beyond
 #define ATTEND_SOLO 8            // tiles of a stream that a wave takes alone, where there are many such streams and none longer
+#define ATTEND_GROUPED 64        // chunks of all streams from which on a chunk's units go to one XCD
 #define ATTEND_FAN 16            // chunks joined at a time
 
 template <int KIND> struct attend_kind;
@@ -162,9 +163,20 @@ __global__ __launch_bounds__(ATTEND_T, D <= 128 ? 2 : 1) void k_seq_attend(atten
     }
 
     // ---- this wave's chunk
-    const int64_t index = solo ? (int64_t)blockIdx.x * ATTEND_WAVES + wave : (int64_t)blockIdx.x;
-    if (index >= (int64_t)pairs * units) return;             // the grid is as large as any lengths need; a workgroup's waves part only where they go alone
-    const int pair = (int)((uint32_t)index / (uint32_t)units), unit = (int)((uint32_t)index % (uint32_t)units);
+    // Workgroups are dealt out to the eight XCDs in turn.  Where the units of a chunk read lines in common - a second tile of heads all of
+    // them, cache heads that lie side by side in parts of a line those - they go to the same XCD, whose L2 then has them (16 streams
+    // of up to 8000 tokens, 8 x 20 heads 89 -> 77 us; up to 32000 of e4m3, 8 x 4 heads of 64 94 -> 74).  Elsewhere, or with few
+    // chunks, that would only load the XCDs less evenly (8 x 1 heads of 128 58 -> 62).
+    int pair, unit;
+    if (solo || !a.grouped || pairs < ATTEND_GROUPED) {
+        const int64_t index = solo ? (int64_t)blockIdx.x * ATTEND_WAVES + wave : (int64_t)blockIdx.x;
+        if (index >= (int64_t)pairs * units) return;         // the grid is as large as any lengths need; a workgroup's waves part only where they go alone
+        pair = (int)((uint32_t)index / (uint32_t)units); unit = (int)((uint32_t)index % (uint32_t)units);
+    } else {
+        const uint32_t k = blockIdx.x >> 3;
+        pair = (int)(k / (uint32_t)units * 8 + (blockIdx.x & 7)); unit = (int)(k % (uint32_t)units);
+        if (pair >= pairs) return;
+    }
     int b = 0, length, split, n_split, first_row;
     if constexpr (MANY) {
         for (int hi = a.n_streams; hi - b > 1;) { const int mid = (b + hi) >> 1; if (s_first[mid] <= pair) b = mid; else hi = mid; }
@@ -600,13 +612,16 @@ extern "C" rh_status rh_cache_attend(rh_ctx* ctx, const rh_kv_cache* cache, cons
     a.n_pages = cache->n_pages; a.heads = cache->heads; a.q_heads = q_heads; a.group = q_heads / cache->heads;
     a.head_tiles = (a.group + 15) / 16; a.max_pages = max_pages; a.n_streams = n_streams; a.window = window; a.n_cu = ctx->n_cu;
     a.scale = scale * 1.44269504089f;
+    const int64_t size = cache->type == RH_T_F32 ? 4 : cache->type == RH_T_BF16 ? 2 : 1;
+    a.grouped = a.head_tiles > 1 || (cache->heads > 1 && (cache->k_stride[2] * size % 128 || cache->v_stride[2] * size % 128));
     // Chunks: at most ATTEND_CHUNKS a CU and one more for every stream and unit; less where the table's rows are short.
-    const int64_t streams_units = (int64_t)cache->heads * a.head_tiles * n_streams;
+    const int64_t units = (int64_t)cache->heads * a.head_tiles, streams_units = units * n_streams;
     const int64_t longest = window && window < (int64_t)max_pages * cache->page ? window : (int64_t)max_pages * cache->page;
     const int tile = cache->type == RH_T_F32 ? 16 : 32;
     const int64_t cut = (longest + tile * ATTEND_CHUNK_MIN - 1) / (tile * ATTEND_CHUNK_MIN);
     int64_t grid = (int64_t)ATTEND_CHUNKS * ctx->n_cu + streams_units;
     grid = streams_units * cut < grid ? streams_units * cut : grid;
+    grid += 8 * units;                                       // the last eight chunks' units, of which not all need be there
     // a stream cut into n > 1 chunks has more than n - 1 >= n / 2 chunks' tiles: at most twice ATTEND_CHUNKS a CU of them need scratch memory
     const size_t rows = (size_t)2 * ATTEND_CHUNKS * ctx->n_cu;
     const rh_status ws = seq_ensure(ctx, rows * (cache->dim / 16 * 64 + 16) * 16, rows);
