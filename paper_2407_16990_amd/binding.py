@@ -157,6 +157,7 @@ def _ptr(t):
 SEQ_TYPE = {torch.float32: 0, torch.bfloat16: 1, torch.float8_e4m3fn: 2}
 _kv_cache = struct.Struct("=4Q6q5i4x").pack          # rh_kv_cache
 _strides2 = struct.Struct("=2q").pack
+_raw_stream = torch._C._cuda_getCurrentRawStream     # handle of torch's current stream
 
 
 class KVCache:
@@ -215,6 +216,7 @@ class RH:
             raise RuntimeError("paper_2407_16990_amd needs a GPU: there is no CPU fallback")
         self.device = torch.device(device)
         torch.cuda.set_device(self.device)
+        self._index = self.device.index or 0
         self.cfg = Config(frame_w, frame_h, max_frames, halo, bin_size, max_bins, connectivity, max_box_mbs,
                           {"fp32": RH_FP32, "bf16": RH_BF16}[precision],
                           NetDesc(TOPOLOGY[net.topology], net.channels, net.n_blocks, net.scale),
@@ -386,7 +388,7 @@ class RH:
     # -- operators of a decode step over many streams (include/rh_seq.h) -------------------------
     def _made(self, *tensors):
         """Outputs made on torch's current stream are held back from reuse until the library's stream, should it be another, is past them."""
-        if torch._C._cuda_getCurrentRawStream(self.device.index or 0) != self._stream.cuda_stream:
+        if _raw_stream(self._index) != self._stream.cuda_stream:
             for t in tensors:
                 if t is not None:
                     t.record_stream(self._stream)
@@ -405,7 +407,7 @@ class RH:
         # one allocation for what is not given
         made = torch.empty(max(n_slots, 0) + 2 * n + 2, dtype=torch.int32, device=self.device)
         self._made(made)
-        slots, new_off, own_lengths, own_count = made.split((max(n_slots, 0), n + 1, n, 1))
+        slots, new_off, own_lengths, own_count = made.split_with_sizes((max(n_slots, 0), n + 1, n, 1))
         new_lengths = own_lengths if new_lengths is None else new_lengths
         new_count = own_count if new_count is None else new_count
         for t, m in ((new_lengths, n), (new_count, 1)):
