@@ -41,7 +41,7 @@ struct attend_args {
 #define ATTEND_CHUNKS 8          // chunks a CU beyond
 #define ATTEND_SOLO 8            // tiles of a stream that a wave takes alone, where there are many such streams and none longer
 #define ATTEND_GROUPED 64        // chunks of all streams from which on a chunk's units go to one XCD
-#define ATTEND_FAN 16            // chunks joined at a time
+#define ATTEND_FAN 16            // chunks joined at a time, at most
 
 template <int KIND> struct attend_kind;
 template <> struct attend_kind<RH_T_F32> { typedef float Q; typedef float C; static constexpr int TT = 1; };
@@ -482,8 +482,10 @@ __global__ __launch_bounds__(ATTEND_T, D <= 128 ? 2 : 1) void k_seq_attend(atten
     uint64_t* rows = (uint64_t*)a.ws + ((size_t)first_row * units + unit) * ROW;
     uint32_t* counts = a.count + (size_t)first_row * units + unit;
     int at = split, members = n_split, stride = 1;           // the row that this workgroup has made, as the at-th of `members`, `stride` rows apart
+    // two levels of about as many each, where one does not do (121 chunks: 25.8 us with groups of 16, 24.9 with 12)
+    const int fan = n_split > ATTEND_FAN && n_split <= 144 ? 12 : ATTEND_FAN;
     for (int level = 0; members > 1; ++level) {
-        const int first = at / ATTEND_FAN * ATTEND_FAN, n = members - first < ATTEND_FAN ? members - first : ATTEND_FAN;
+        const int first = at / fan * fan, n = members - first < fan ? members - first : fan;
         if (n > 1) {
             if (wave == 0) {
                 uint64_t* o = rows + (size_t)at * stride * step;
@@ -500,7 +502,7 @@ __global__ __launch_bounds__(ATTEND_T, D <= 128 ? 2 : 1) void k_seq_attend(atten
                 }
                 asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
                 if (lane == 0) {
-                    // a group of a higher level holds more than ATTEND_FAN rows: a counter of its own beside the lower levels'
+                    // a group of a higher level holds more than fan rows: a counter of its own beside the lower levels'
                     uint32_t* count = counts + (size_t)(first * stride + level) * units;
                     const bool last = __hip_atomic_fetch_add(count, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)n - 1;
                     if (last) __hip_atomic_store(count, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -540,7 +542,7 @@ __global__ __launch_bounds__(ATTEND_T, D <= 128 ? 2 : 1) void k_seq_attend(atten
                     if (quarter < 4) s_acc[0][NT][quarter * 16 + h] = f32x4{m, tot, 0.f, 0.f};
                 }
             };
-            if (n <= 4) join_rows(seq_const<4>()); else join_rows(seq_const<ATTEND_FAN>());
+            if (n <= 4) join_rows(seq_const<4>()); else if (n <= 12) join_rows(seq_const<12>()); else join_rows(seq_const<ATTEND_FAN>());
             __syncthreads();
             if (wave == 0) {
 #pragma unroll
@@ -549,7 +551,7 @@ __global__ __launch_bounds__(ATTEND_T, D <= 128 ? 2 : 1) void k_seq_attend(atten
                 top = stat[0]; total = stat[1];
             }
         }
-        at /= ATTEND_FAN; members = (members + ATTEND_FAN - 1) / ATTEND_FAN; stride *= ATTEND_FAN;
+        at /= fan; members = (members + fan - 1) / fan; stride *= fan;
     }
     if (wave == 0 || solo) write();
 }
