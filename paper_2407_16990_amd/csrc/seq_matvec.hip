@@ -91,17 +91,19 @@ __global__ __launch_bounds__(64 * MATVEC_WAVES(XT, MT)) void k_seq_matvec(matvec
     extern __shared__ uint4 s_mem[];
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6, c = lane & 15, j = lane >> 4;
     const int tw = wave / a.ks, ks = wave % a.ks;
-    const int m0 = blockIdx.y * 16 * MT, M = a.rows - m0 < 16 * MT ? a.rows - m0 : 16 * MT;
-    // x in LDS: pieces of 16 bytes, [part][step][as the lanes of a product read them][row]
-    const int part_pieces = a.chunk * 4 * PER_STEP * M;
+    const int m0 = blockIdx.y * 16 * MT, M = a.rows - m0 < 16 * MT ? a.rows - m0 : 16 * MT, P = M | 1;
+    // x in LDS: pieces of 16 bytes, [part][step][as the lanes of a product read them][row]; an odd number P of rows, or neighbouring
+    // pieces of a row would be written to the same banks (16 x 4096 x 4096, bf16 rows: 8.4 -> 6.9 us)
+    const int part_pieces = a.chunk * 4 * PER_STEP * P;
     u32x4* xs = (u32x4*)s_mem;
-    f32x4* s_sum = (f32x4*)(xs + PARTS * part_pieces);       // [wave][R * MT][lane]
+    // the waves' sums [wave][R * MT][lane]: behind x, or in its place where x does not lie here as a whole
+    f32x4* s_sum = (f32x4*)(a.chunk < a.quads ? xs : xs + PARTS * part_pieces);
 
     constexpr int W = PIECE * sizeof(T) / 4;                 // words of a piece in memory
     auto put = [&](int m, int p, const uint32_t* v) {        // piece p of row m
         // bf16: lane quarter j of the e-th product of a step reads block j's piece e; the scaled product has pieces j and 4 + j there
         const int step = p / PER_STEP, in = p % PER_STEP;
-        u32x4* to = xs + (step * PER_STEP + (XT == MATVEC_SCALED ? in : in % 4 * 4 + in / 4)) * M + m;
+        u32x4* to = xs + (step * PER_STEP + (XT == MATVEC_SCALED ? in : in % 4 * 4 + in / 4)) * P + m;
         if constexpr (XT == RH_T_F32) {
             uint32_t w[3][4];
 #pragma unroll
@@ -212,17 +214,17 @@ __global__ __launch_bounds__(64 * MATVEC_WAVES(XT, MT)) void k_seq_matvec(matvec
     f32x4 acc[R][MT];
     int mrow[MT];                                            // rows that are none read row 0
 #pragma unroll
-    for (int i = 0; i < MT; ++i) mrow[i] = j * M + (16 * i + c < M ? 16 * i + c : 0);
+    for (int i = 0; i < MT; ++i) mrow[i] = j * P + (16 * i + c < M ? 16 * i + c : 0);
 
     auto multiply = [&](const weights& w, int q) {
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
-            const u32x4* x = xs + (q * 4 + s) * PER_STEP * M;
+            const u32x4* x = xs + (q * 4 + s) * PER_STEP * P;
             if constexpr (XT == MATVEC_SCALED) {
                 i32x8 xb[MT];
 #pragma unroll
                 for (int i = 0; i < MT; ++i) {
-                    const u32x4 lo = x[mrow[i]], hi = x[4 * M + mrow[i]];
+                    const u32x4 lo = x[mrow[i]], hi = x[4 * P + mrow[i]];
                     xb[i] = i32x8{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
                 }
 #pragma unroll
@@ -249,7 +251,7 @@ __global__ __launch_bounds__(64 * MATVEC_WAVES(XT, MT)) void k_seq_matvec(matvec
                         for (int p = PARTS - 1; p >= 0; --p)
 #pragma unroll
                             for (int i = 0; i < MT; ++i) {
-                                const bf16x8 xb = __builtin_bit_cast(bf16x8, x[p * part_pieces + e * 4 * M + mrow[i]]);
+                                const bf16x8 xb = __builtin_bit_cast(bf16x8, x[p * part_pieces + e * 4 * P + mrow[i]]);
 #pragma unroll
                                 for (int r = 0; r < R; ++r) acc[r][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wa[r], xb, acc[r][i], 0, 0, 0);
                             }
@@ -271,7 +273,7 @@ __global__ __launch_bounds__(64 * MATVEC_WAVES(XT, MT)) void k_seq_matvec(matvec
                             for (int p = PARTS - 1; p >= 0; --p)
 #pragma unroll
                                 for (int i = 0; i < MT; ++i)
-                                    part[r][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wa, __builtin_bit_cast(bf16x8, x[p * part_pieces + e * 4 * M + mrow[i]]), part[r][i], 0, 0, 0);
+                                    part[r][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wa, __builtin_bit_cast(bf16x8, x[p * part_pieces + e * 4 * P + mrow[i]]), part[r][i], 0, 0, 0);
                         }
 #pragma unroll
                     for (int r = 0; r < R; ++r)
@@ -354,6 +356,7 @@ __global__ __launch_bounds__(64 * MATVEC_WAVES(XT, MT)) void k_seq_matvec(matvec
 #pragma unroll
                         for (int i = 0; i < MT; ++i) acc[r][i] += s_sum[((wave + k) * R * MT + r * MT + i) * 64 + lane];
             }
+            if (a.chunk < a.quads) staged = a.quads;         // no chunk: the sums lie there
         }
         if (!ks && tile < a.tiles) write(tile);
     }
@@ -369,11 +372,12 @@ static hipError_t launch_matvec(rh_ctx* ctx, matvec_args a)
         if (e != hipSuccess) return e;
         attr_done[ctx->device] = true;
     }
-    const int M = a.rows < 16 * MT ? a.rows : 16 * MT, quad = K::PARTS * 512 / K::PIECE * 16 * M;       // bytes of x in LDS, of a stretch
+    const int M = a.rows < 16 * MT ? a.rows : 16 * MT, quad = K::PARTS * 512 / K::PIECE * 16 * (M | 1);       // bytes of x in LDS, of a stretch
     constexpr int WAVES = MATVEC_WAVES(XT, MT), sums = WAVES * R * MT * 64 * (int)sizeof(f32x4);
     a.quads = (a.ins + 511) / 512;
-    a.chunk = (MATVEC_LDS - sums) / quad;
-    a.chunk = a.chunk < a.quads ? a.chunk : a.quads;
+    const bool whole = a.quads * (int64_t)quad + sums <= MATVEC_LDS;
+    a.chunk = whole ? a.quads : MATVEC_LDS / quad < a.quads - 1 ? MATVEC_LDS / quad : a.quads - 1;
+    a.chunk = a.chunk < 1 ? 1 : a.chunk;
     a.tiles = (a.outs + 16 * R - 1) / (16 * R);
     a.row_pieces[0] = seq_make_div(a.chunk * (512 / K::PIECE));
     a.row_pieces[1] = seq_make_div(a.quads % a.chunk ? a.quads % a.chunk * (512 / K::PIECE) : 1);
@@ -386,7 +390,7 @@ static hipError_t launch_matvec(rh_ctx* ctx, matvec_args a)
     while (a.ks * a.tw < WAVES && a.ks < a.chunk) a.ks *= 2;
     const int groups = (a.tiles + a.tw - 1) / a.tw;
     hipLaunchKernelGGL((k_seq_matvec<XT, MT, R>), dim3(groups < wgs ? groups : wgs, (a.rows + 16 * MT - 1) / (16 * MT)), dim3(64 * a.tw * a.ks),
-                       (size_t)a.chunk * quad + (a.ks > 1 ? sums : 0), ctx->stream, a);
+                       whole ? (size_t)a.quads * quad + (a.ks > 1 ? sums : 0) : MATVEC_LDS, ctx->stream, a);
     return hipGetLastError();
 }
 
@@ -407,7 +411,7 @@ extern "C" rh_status rh_matvec_packed(rh_ctx* ctx, const void* x, int32_t x_type
     matvec_args a = {};
     a.x = x; a.x_scale = x_scale; a.w = w; a.w_scale = w_scale; a.y = y; a.x_stride = x_stride; a.y_stride = y_stride;
     a.rows = n_rows; a.outs = n_out; a.ins = n_in; a.blocks = (n_in + 31) / 32; a.relu = relu; a.y_f32 = y_type == RH_T_F32;
-    // More rows a pass read the weights fewer times; what x takes of the LDS bounds them.
+    // Rows a pass: more read the weights fewer times; what x takes of the LDS, and sums of registers, bounds them.
     hipError_t e;
     if (x_type == RH_T_F32) e = launch_matvec<RH_T_F32, 1, 1>(ctx, a);
     else if (x_type == RH_T_BF16) e = n_rows <= 16 ? launch_matvec<RH_T_BF16, 1, 1>(ctx, a) : launch_matvec<RH_T_BF16, 2, 2>(ctx, a);
