@@ -11,9 +11,8 @@
  * They take a context of rh.h and follow its conventions: device pointers, caller-owned buffers, all work on the context's
  * stream, arguments checked before any launch, rh_last_error.  They use neither the context's network nor its capacities,
  * and count in no class of rh_profile_read.  Sums, softmax statistics and norms are held in 32 bits.
- * Scratch memory of rh_cache_attend belongs to the context and only grows: a call that needs more than every earlier one
- * synchronises the stream and reallocates it; what it needs follows from the head size alone, so that after one call a graph of calls
- * with heads as large may be captured.  rh_cache_plan has a counter there, which any first call of either makes.  The others need none.
+ * Scratch memory of rh_cache_attend (68 MB on 256 CUs) and a few counters, of rh_cache_plan too, belong to the context: the first call that wants
+ * them allocates them, no later one allocates or synchronises, so that from then on calls may be captured into graphs.
  */
 #ifndef RH_SEQ_H
 #define RH_SEQ_H

@@ -110,11 +110,9 @@ struct rh_ctx {
     // enhance workspace (grow-only)
     void* act;
     size_t act_bytes;
-    // operators of rh_seq.h: partial results (grow-only), and counters that are zero between calls
+    // operators of rh_seq.h, made at the first call that wants them: partial results, and counters that are zero between calls
     void* seq_ws;
-    size_t seq_bytes;
     uint32_t* seq_cnt;
-    size_t seq_n;
 };
 
 #define RH_FAIL(ctx, code, ...)                                           \

@@ -37,8 +37,7 @@ struct attend_args {
 #define ATTEND_WAVES 4
 #define ATTEND_T (64 * ATTEND_WAVES)
 #define ATTEND_CHUNK_MIN 4       // tiles
-#define ATTEND_CHUNK_FEW 32      // tiles a chunk up to which each CU gets one chunk
-#define ATTEND_CHUNKS 8          // chunks a CU beyond
+#define ATTEND_CHUNK_FEW 32      // tiles a chunk up to which each CU gets one chunk; beyond, ATTEND_CHUNKS
 #define ATTEND_SOLO 8            // tiles of a stream that a wave takes alone, where there are many such streams and none longer
 #define ATTEND_GROUPED 64        // chunks of all streams from which on a chunk's units go to one XCD
 #define ATTEND_FAN 16            // chunks joined at a time, at most
@@ -477,7 +476,7 @@ __global__ __launch_bounds__(ATTEND_T, D <= 128 ? 2 : 1) void k_seq_attend(atten
     // loaded past the L2, and a wave's stores are acknowledged before the chunk is counted.  (Fences, which write the whole L2 back, took
     // 490 of 690 us on 64 x 8192 tokens.)
     struct two { uint64_t u[2]; };
-    constexpr int ROW = (NT * 64 + 16) * 2;                  // words of 8 bytes: sums of 16 heads, and their maxima and totals
+    constexpr int ROW = SEQ_ROW_BYTES(D) / 8;                // words of a row
     const size_t step = (size_t)units * ROW;
     uint64_t* rows = (uint64_t*)a.ws + ((size_t)first_row * units + unit) * ROW;
     uint32_t* counts = a.count + (size_t)first_row * units + unit;
@@ -624,9 +623,8 @@ extern "C" rh_status rh_cache_attend(rh_ctx* ctx, const rh_kv_cache* cache, cons
     int64_t grid = (int64_t)ATTEND_CHUNKS * ctx->n_cu + streams_units;
     grid = streams_units * cut < grid ? streams_units * cut : grid;
     grid += 8 * units;                                       // the last eight chunks' units, of which not all need be there
-    // a stream cut into n > 1 chunks has more than n - 1 >= n / 2 chunks' tiles: at most twice ATTEND_CHUNKS a CU of them need scratch memory
-    const size_t rows = (size_t)2 * ATTEND_CHUNKS * ctx->n_cu;
-    const rh_status ws = seq_ensure(ctx, rows * (cache->dim / 16 * 64 + 16) * 16, rows);
+    rh_status ws = seq_counters(ctx);
+    if (ws == RH_OK) ws = seq_scratch(ctx);
     if (ws != RH_OK) return ws;
     a.ws = (float*)ctx->seq_ws; a.count = ctx->seq_cnt;
     RH_HIP(ctx, cache->type == RH_T_F32 ? launch_attend<RH_T_F32>(ctx, a, grid, cache->dim)

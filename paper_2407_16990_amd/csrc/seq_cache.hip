@@ -183,7 +183,7 @@ rh_status rh_launch_cache_plan(rh_ctx* ctx, plan_args& a)
     const int64_t wgs = (int64_t)a.n_slots / PLAN_SLOTS + (int64_t)a.n_streams * a.max_pages / PLAN_PAGES;
     const int grid = (int)(wgs < 1 ? 1 : wgs < PLAN_A_CU * ctx->n_cu ? wgs : PLAN_A_CU * ctx->n_cu);
     if (grid > 1 && (a.new_lengths == a.lengths || a.new_count == a.free_count)) {
-        const rh_status st = seq_ensure(ctx, 0, 1);
+        const rh_status st = seq_counters(ctx);
         if (st != RH_OK) return st;
         a.ticket = ctx->seq_cnt;
     }
@@ -362,24 +362,23 @@ __global__ void k_seq_zero(uint32_t* p, uint32_t n)
     if (i < n) p[i] = 0;
 }
 
-rh_status seq_ensure(rh_ctx* ctx, size_t bytes, size_t counters)
+// Both are made once, at their full size, at the first call that wants them: what a graph has recorded stays where it is.
+rh_status seq_counters(rh_ctx* ctx)
 {
-    if (bytes > ctx->seq_bytes) {
-        RH_HIP(ctx, hipStreamSynchronize(ctx->stream));
-        if (ctx->seq_ws) { (void)hipFree(ctx->seq_ws); ctx->seq_ws = nullptr; ctx->seq_bytes = 0; }
-        if (hipMalloc(&ctx->seq_ws, bytes) != hipSuccess) { ctx->seq_ws = nullptr; RH_FAIL(ctx, RH_E_NOMEM, "scratch memory of %zu bytes", bytes); }
-        ctx->seq_bytes = bytes;
-    }
-    if (counters > ctx->seq_n) {
-        const size_t n = counters < 1024 ? 1024 : counters;
-        RH_HIP(ctx, hipStreamSynchronize(ctx->stream));
-        if (ctx->seq_cnt) { (void)hipFree(ctx->seq_cnt); ctx->seq_cnt = nullptr; ctx->seq_n = 0; }
-        if (hipMalloc((void**)&ctx->seq_cnt, n * sizeof(uint32_t)) != hipSuccess) { ctx->seq_cnt = nullptr; RH_FAIL(ctx, RH_E_NOMEM, "%zu counters", n); }
-        // A fill kernel that fails leaves no counters behind: the next call would trust them to be zero.
-        hipLaunchKernelGGL(k_seq_zero, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, ctx->stream, ctx->seq_cnt, (uint32_t)n);
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) { (void)hipFree(ctx->seq_cnt); ctx->seq_cnt = nullptr; RH_FAIL(ctx, RH_E_DEVICE, "clearing counters: %s", hipGetErrorString(e)); }
-        ctx->seq_n = n;
-    }
+    if (ctx->seq_cnt) return RH_OK;
+    const uint32_t n = (uint32_t)SEQ_ROWS(ctx);
+    if (hipMalloc((void**)&ctx->seq_cnt, n * sizeof(uint32_t)) != hipSuccess) { ctx->seq_cnt = nullptr; RH_FAIL(ctx, RH_E_NOMEM, "%u counters", n); }
+    // A fill kernel that was lost leaves no counters behind: the next call would trust them to be zero.
+    hipLaunchKernelGGL(k_seq_zero, dim3((n + 255) / 256), dim3(256), 0, ctx->stream, ctx->seq_cnt, n);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) { (void)hipFree(ctx->seq_cnt); ctx->seq_cnt = nullptr; RH_FAIL(ctx, RH_E_DEVICE, "clearing counters: %s", hipGetErrorString(e)); }
+    return RH_OK;
+}
+
+rh_status seq_scratch(rh_ctx* ctx)
+{
+    if (ctx->seq_ws) return RH_OK;
+    const size_t bytes = (size_t)SEQ_ROWS(ctx) * SEQ_ROW_BYTES(RH_SEQ_MAX_DIM);
+    if (hipMalloc(&ctx->seq_ws, bytes) != hipSuccess) { ctx->seq_ws = nullptr; RH_FAIL(ctx, RH_E_NOMEM, "scratch memory of %zu bytes", bytes); }
     return RH_OK;
 }

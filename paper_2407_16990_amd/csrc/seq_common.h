@@ -84,7 +84,13 @@ inline seq_div seq_make_div(uint32_t d)
 }
 __device__ __forceinline__ uint32_t seq_quot(uint32_t x, const seq_div& v) { return (__umulhi(x, v.m) + (x & v.one)) >> v.s; }
 
-// scratch memory of rh_cache_attend: partial results, and counters that are zero between calls
-rh_status seq_ensure(rh_ctx* ctx, size_t bytes, size_t counters);
+// Scratch memory: rows of partial results of rh_cache_attend, and as many counters, which are zero between calls (rh_cache_plan takes the
+// first).  A stream cut into n > 1 chunks has more than n - 1 >= n / 2 chunks' tiles, so that of ATTEND_CHUNKS chunks a CU twice as many at most
+// belong to such streams.
+#define ATTEND_CHUNKS 8          // chunks a CU of rh_cache_attend
+#define SEQ_ROWS(ctx) (2 * ATTEND_CHUNKS * (ctx)->n_cu)
+#define SEQ_ROW_BYTES(dim) (((dim) / 16 * 64 + 16) * 16)     // sums of 16 heads, and a maximum and a total of each
+rh_status seq_counters(rh_ctx* ctx);
+rh_status seq_scratch(rh_ctx* ctx);
 // refusals of a cache; `name` is the call's
 rh_status seq_check_cache(rh_ctx* ctx, const char* name, const rh_kv_cache* c);

@@ -294,7 +294,8 @@ def test_attend_window(rh, q_dtype, c_dtype, window):
 
 
 @pytest.mark.parametrize("q_dtype,c_dtype", KINDS)
-@pytest.mark.parametrize("n,length,heads,group", [(1, 30000, 1, 1), (1, 20001, 2, 8), (3, 9000, 1, 20), (60, 300, 8, 2), (300, 40, 4, 1)])
+@pytest.mark.parametrize("n,length,heads,group", [(1, 30000, 1, 1), (1, 20001, 2, 8), (3, 9000, 1, 20), (60, 300, 8, 2), (300, 40, 4, 1),
+                                                    (64, 30, 8, 2), (64, 100, 16, 1), (100, 5000, 2, 4), (8, 12000, 2, 20), (2048, 20, 2, 1), (65, 1000, 1, 17)])
 def test_attend_split_and_joined(rh, q_dtype, c_dtype, n, length, heads, group):
     """One long stream among short ones, and many: whatever the split, and the same bits on every run."""
     lens = [length] + [(7 * i * length // n) % (length // 3) for i in range(1, n)]
@@ -304,6 +305,18 @@ def test_attend_split_and_joined(rh, q_dtype, c_dtype, n, length, heads, group):
     for _ in range(4):
         again = rh.cache_attend(q, cache, table, lengths, want_lse=True)
         assert torch.equal(out, again[0]) and torch.equal(lse, again[1])
+
+
+@pytest.mark.parametrize("q_dtype,c_dtype", KINDS)
+@pytest.mark.parametrize("dim,heads,group", [(96, 4, 3), (32, 3, 1), (64, 5, 18)])
+def test_attend_many_chunks_of_heads_that_share_lines(rh, q_dtype, c_dtype, dim, heads, group):
+    lens = [3000 + 211 * i for i in range(20)] + [0, 1, 17]
+    q, cache, table, lengths = _attend_inputs(dim, lens, heads, group, dim, 16, q_dtype, c_dtype, "token")
+    got = rh.cache_attend(q, cache, table, lengths, want_lse=True)
+    again = rh.cache_attend(q, cache, table, lengths, want_lse=True)
+    assert torch.equal(got[0], again[0]) and torch.equal(got[1], again[1])
+    pick = [0, 7, 19, 20, 21, 22]                              # the reference takes its time: some of the streams
+    _check_attend(rh, q[pick], cache, table[pick].contiguous(), lengths[pick].contiguous(), dim ** -0.5, got=(got[0][pick], got[1][pick]))
 
 
 @pytest.mark.parametrize("q_dtype,c_dtype", KINDS)
@@ -480,7 +493,8 @@ TYPES = [torch.float32, torch.bfloat16, E4M3]
 
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("rows,n_out,n_in", [(1, 1, 1), (1, 16, 32), (1, 17, 31), (2, 5, 33), (3, 100, 127), (1, 64, 129), (5, 33, 510), (16, 1024, 512), (17, 130, 920),
-                                             (1, 4096, 1024), (33, 200, 300), (64, 96, 2048), (65, 70, 700), (130, 40, 64), (4, 2, 8192), (1, 500, 16384), (8, 48, 20000), (15, 1, 511)])
+                                             (1, 4096, 1024), (33, 200, 300), (64, 96, 2048), (65, 70, 700), (130, 40, 64), (4, 2, 8192), (1, 500, 16384), (8, 48, 20000), (15, 1, 511),
+                                             (64, 9000, 2100), (16, 5000, 2048), (24, 8300, 3500)])
 def test_matvec(rh, dtype, rows, n_out, n_in):
     g = torch.Generator(device="cuda").manual_seed(rows * 7 + n_out * 3 + n_in)
     w, sc = _weights(g, n_out, n_in)
