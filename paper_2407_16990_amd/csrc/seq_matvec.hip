@@ -312,7 +312,8 @@ __global__ __launch_bounds__(64 * MATVEC_WAVES(XT, MT)) void k_seq_matvec(matvec
 
     place at = {(int)blockIdx.x * a.tw + tw, 0, 0, 0};
     weights now, next;
-    bool have = at.tile < a.tiles;
+    const bool idle = tw >= a.tw;                            // waves that only help to lay x out
+    bool have = !idle && at.tile < a.tiles;
     if (have) {
         share(at);
         if (at.q >= at.end) { at.q = at.end; have = advance(at); }
@@ -342,14 +343,14 @@ __global__ __launch_bounds__(64 * MATVEC_WAVES(XT, MT)) void k_seq_matvec(matvec
         }
         if (a.ks > 1) {
             __syncthreads();                                 // the sums of the round before have been read
-            if (ks) {
+            if (ks && !idle) {
 #pragma unroll
                 for (int r = 0; r < R; ++r)
 #pragma unroll
                     for (int i = 0; i < MT; ++i) s_sum[(wave * R * MT + r * MT + i) * 64 + lane] = acc[r][i];
             }
             __syncthreads();
-            if (!ks) {
+            if (!ks && !idle) {
                 for (int k = 1; k < a.ks; ++k)
 #pragma unroll
                     for (int r = 0; r < R; ++r)
@@ -358,7 +359,7 @@ __global__ __launch_bounds__(64 * MATVEC_WAVES(XT, MT)) void k_seq_matvec(matvec
             }
             if (a.chunk < a.quads) staged = a.quads;         // no chunk: the sums lie there
         }
-        if (!ks && tile < a.tiles) write(tile);
+        if (!ks && !idle && tile < a.tiles) write(tile);
     }
 }
 
@@ -389,7 +390,11 @@ static hipError_t launch_matvec(rh_ctx* ctx, matvec_args a)
     a.ks = 1;
     while (a.ks * a.tw < WAVES && a.ks < a.chunk) a.ks *= 2;
     const int groups = (a.tiles + a.tw - 1) / a.tw;
-    hipLaunchKernelGGL((k_seq_matvec<XT, MT, R>), dim3(groups < wgs ? groups : wgs, (a.rows + 16 * MT - 1) / (16 * MT)), dim3(64 * a.tw * a.ks),
+    // and as many more as have eight pieces of x each to lay out
+    const int64_t pieces = (int64_t)a.chunk * (512 / K::PIECE) * M;
+    int waves = a.tw * a.ks;
+    while (waves < WAVES && (int64_t)waves * 64 * 8 <= pieces) ++waves;
+    hipLaunchKernelGGL((k_seq_matvec<XT, MT, R>), dim3(groups < wgs ? groups : wgs, (a.rows + 16 * MT - 1) / (16 * MT)), dim3(64 * waves),
                        whole ? (size_t)a.quads * quad + (a.ks > 1 ? sums : 0) : MATVEC_LDS, ctx->stream, a);
     return hipGetLastError();
 }
