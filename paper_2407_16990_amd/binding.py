@@ -1,11 +1,11 @@
-"""ctypes binding of librh.so.  Argument marshalling only: every step of the path runs in the
+"""ctypes binding of librh.so (the sequence operators' through _seq.so, in C++).  Argument marshalling only: every step of the path runs in the
 library's HIP kernels.  torch supplies device memory and the stream.  There is no fallback:
 if the library is missing or a call fails, an exception is raised."""
 from __future__ import annotations
 
 import ctypes as C
+import importlib.util
 import os
-import struct
 from dataclasses import dataclass
 
 import numpy as np
@@ -56,13 +56,14 @@ def lib_path() -> str:
 
 
 _lib = None
+_seq = None            # _seq.so: the sequence operators on torch tensors (csrc/seq_binding.cpp)
 
 
 def _library_is_stale(path: str) -> bool:
     """True when librh.so is missing or was built from other sources than the ones in the tree
     (build.py records a digest of csrc/ and include/ beside the library)."""
     from . import build as _b
-    if not os.path.exists(path) or not os.path.exists(_b.STAMP):
+    if not os.path.exists(path) or not os.path.exists(_b.STAMP) or not os.path.exists(_b.MODULE):
         return True
     with open(_b.STAMP) as f:
         return f.read().strip() != _b.source_digest()
@@ -70,7 +71,7 @@ def _library_is_stale(path: str) -> bool:
 
 def load_library():
     """Load librh.so; it is built first when it is missing or a source file is newer than it."""
-    global _lib
+    global _lib, _seq
     if _lib is not None:
         return _lib
     path = lib_path()
@@ -110,6 +111,10 @@ def load_library():
     L.rh_norm_residual.argtypes = [vp, vp, i64, vp, i64, vp, i32, i32, i32, f32, vp, i64, vp, vp, vp]
     L.rh_matvec_packed.argtypes = [vp, vp, i32, i64, vp, vp, vp, i32, i32, i32, i32, vp, i32, i64]
     L.rh_select_regions_noalloc.argtypes = [vp, i32, i32, i32, C.POINTER(Segment), i32, i32, vp, vp, vp, vp]
+    spec = importlib.util.spec_from_file_location("_seq", os.path.join(_HERE, "_seq.so"))
+    _seq = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(_seq)
+    _seq.init(*[C.cast(f, vp).value for f in (L.rh_cache_plan, L.rh_cache_write, L.rh_cache_attend, L.rh_norm_residual, L.rh_matvec_packed)])
     _lib = L
     return L
 
@@ -153,10 +158,6 @@ def _ptr(t):
     return None if t is None else C.c_void_p(t.data_ptr())
 
 
-# element types of the sequence operators (include/rh_seq.h), and what the calls take by pointer, as bytes
-SEQ_TYPE = {torch.float32: 0, torch.bfloat16: 1, torch.float8_e4m3fn: 2}
-_kv_cache = struct.Struct("=4Q6q5i4x").pack          # rh_kv_cache
-_strides2 = struct.Struct("=2q").pack
 _raw_stream = torch._C._cuda_getCurrentRawStream     # handle of torch's current stream
 
 
@@ -166,17 +167,26 @@ class KVCache:
     [n_pages, heads, page] for float8_e4m3fn, else None."""
 
     def __init__(self, k, v, k_scale=None, v_scale=None):
-        shape, ks, vs = k.shape, k.stride(), v.stride()
-        assert k.is_cuda and v.is_cuda and k.dtype == v.dtype and len(shape) == 4 and v.shape == shape
-        assert ks[3] == 1 and vs[3] == 1, "the elements of a head lie side by side"
-        n_pages, page, heads, dim = shape
-        for sc in (k_scale, v_scale):
-            assert sc is None or (sc.is_cuda and sc.dtype == torch.float32 and sc.is_contiguous() and sc.shape == (n_pages, heads, page))
+        if _seq is None:
+            load_library()
+        self.desc = _seq.kv_desc(k, v, k_scale, v_scale)           # rh_kv_cache
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
-        self.n_pages, self.page, self.heads, self.dim = n_pages, page, heads, dim
-        self.desc = _kv_cache(k.data_ptr(), v.data_ptr(), k_scale.data_ptr() if k_scale is not None else 0,
-                              v_scale.data_ptr() if v_scale is not None else 0, ks[0], ks[1], ks[2], vs[0], vs[1], vs[2],
-                              SEQ_TYPE[k.dtype], n_pages, page, heads, dim)
+
+    @property
+    def n_pages(self) -> int:
+        return self.k.shape[0]
+
+    @property
+    def page(self) -> int:
+        return self.k.shape[1]
+
+    @property
+    def heads(self) -> int:
+        return self.k.shape[2]
+
+    @property
+    def dim(self) -> int:
+        return self.k.shape[3]
 
 
 def pack_weights(w) -> tuple:
@@ -231,11 +241,12 @@ class RH:
         if st != 0:
             raise RhError(st, "rh_create failed (see include/rh.h for the limits)")
         self.h = h
+        self._ctx = h.value                                        # for _seq
 
     def close(self):
         if getattr(self, "h", None):
             self.lib.rh_destroy(self.h)
-            self.h = None
+            self.h, self._ctx = None, 0
 
     __del__ = close
 
@@ -386,12 +397,16 @@ class RH:
         return importance
 
     # -- operators of a decode step over many streams (include/rh_seq.h) -------------------------
-    def _made(self, *tensors):
-        """Outputs made on torch's current stream are held back from reuse until the library's stream, should it be another, is past them."""
-        if _raw_stream(self._index) != self._stream.cuda_stream:
-            for t in tensors:
+    def _outputs(self, got):
+        """What a call of _seq returned: a status (0 aside) raises.  Outputs, made on torch's current stream, are held back from
+        reuse until the library's stream, should it be another, is past them."""
+        if type(got) is int:
+            self._check(got)
+        elif _raw_stream(self._index) != self._stream.cuda_stream:
+            for t in got if type(got) is tuple else (got,):
                 if t is not None:
                     t.record_stream(self._stream)
+        return got
 
     def cache_plan(self, n_new: torch.Tensor, lengths: torch.Tensor, block_table: torch.Tensor, free_pages: torch.Tensor,
                    free_count: torch.Tensor, page: int, n_slots: int, new_lengths: torch.Tensor | None = None,
@@ -399,99 +414,31 @@ class RH:
         """Room for the next tokens: block_table [n_streams, max_pages] and free_pages [n_pages] are updated in place.
         -> (slots int32 [n_slots], new_off int32 [n_streams + 1], new_lengths int32 [n_streams], new_count int32 [1]);
         new_lengths / new_count may be given, lengths / free_count themselves among others."""
-        n = n_new.numel()
-        for t in (n_new, lengths, block_table, free_pages, free_count):
-            assert t.is_cuda and t.dtype == torch.int32 and t.is_contiguous()
-        width = block_table.shape
-        assert lengths.numel() == n and len(width) == 2 and width[0] == n and free_count.numel() == 1
-        # one allocation for what is not given
-        made = torch.empty(max(n_slots, 0) + 2 * n + 2, dtype=torch.int32, device=self.device)
-        self._made(made)
-        slots, new_off, own_lengths, own_count = made.split_with_sizes((max(n_slots, 0), n + 1, n, 1))
-        new_lengths = own_lengths if new_lengths is None else new_lengths
-        new_count = own_count if new_count is None else new_count
-        for t, m in ((new_lengths, n), (new_count, 1)):
-            assert t.is_cuda and t.dtype == torch.int32 and t.is_contiguous() and t.numel() == m
-        self._check(self.lib.rh_cache_plan(self.h, n_new.data_ptr(), lengths.data_ptr(), n, page, free_pages.numel(), width[1],
-                                           block_table.data_ptr(), free_pages.data_ptr(), free_count.data_ptr(), slots.data_ptr(), n_slots,
-                                           new_off.data_ptr(), new_lengths.data_ptr(), new_count.data_ptr()))
-        return slots, new_off, new_lengths, new_count
+        return self._outputs(_seq.cache_plan(self._ctx, n_new, lengths, block_table, free_pages, free_count, page, n_slots, new_lengths, new_count))
 
     def cache_write(self, cache: KVCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor) -> None:
         """k, v [n, heads, dim] (float32 or bfloat16, last stride 1) of n tokens into their slots int32 [n]; -1: skipped."""
-        n, ks, vs = slots.numel(), k.stride(), v.stride()
-        assert k.is_cuda and v.is_cuda and k.dtype == v.dtype and k.shape == v.shape == (n, cache.heads, cache.dim)
-        assert ks[2] == 1 and vs[2] == 1 and slots.is_cuda and slots.dtype == torch.int32 and slots.is_contiguous()
-        self._check(self.lib.rh_cache_write(self.h, cache.desc, k.data_ptr(), _strides2(ks[0], ks[1]), v.data_ptr(),
-                                            _strides2(vs[0], vs[1]), SEQ_TYPE[k.dtype], slots.data_ptr(), n))
+        self._check(_seq.cache_write(self._ctx, cache.desc, k, v, slots))
 
     def cache_attend(self, q: torch.Tensor, cache: KVCache, block_table: torch.Tensor, lengths: torch.Tensor,
                      scale: float | None = None, window: int = 0, out: torch.Tensor | None = None, want_lse: bool = False):
         """q [n_streams, q_heads, dim], one token a stream, over lengths[b] cached tokens -> out [n_streams, q_heads, dim]
         (with want_lse: and lse f32 [n_streams, q_heads]).  scale None: dim ** -0.5; window 0: all tokens."""
-        shape, qs, width = q.shape, q.stride(), block_table.shape
-        n, heads, dim = shape
-        assert q.is_cuda and qs[2] == 1 and dim == cache.dim
-        assert block_table.is_cuda and block_table.dtype == torch.int32 and block_table.is_contiguous() and len(width) == 2 and width[0] == n
-        assert lengths.is_cuda and lengths.dtype == torch.int32 and lengths.is_contiguous() and lengths.numel() == n
-        given = out is not None
-        if not given:
-            out = torch.empty(shape, dtype=q.dtype, device=self.device)
-        assert not given or (out.is_cuda and out.dtype == q.dtype and out.is_contiguous() and out.shape == shape)
-        lse = torch.empty((n, heads), dtype=torch.float32, device=self.device) if want_lse else None
-        self._made(None if given else out, lse)
-        self._check(self.lib.rh_cache_attend(self.h, cache.desc, q.data_ptr(), _strides2(qs[0], qs[1]), SEQ_TYPE[q.dtype], heads,
-                                             block_table.data_ptr(), width[1], lengths.data_ptr(), n,
-                                             dim ** -0.5 if scale is None else scale, window, out.data_ptr(),
-                                             lse.data_ptr() if want_lse else None))
-        return (out, lse) if want_lse else out
+        got = self._outputs(_seq.cache_attend(self._ctx, cache.desc, q, block_table, lengths, scale, window, out, want_lse))
+        return got if want_lse else got[0]
 
     def norm_residual(self, x: torch.Tensor, weight: torch.Tensor, residual: torch.Tensor | None = None, eps: float = 1e-6,
                       outputs: str = "same", sum_out: torch.Tensor | None = None):
         """x [rows, cols] (+ residual), normed by its root mean square and weighted -> (sum, y, y8, y8_scale), None where not
         asked for: sum with a residual (into sum_out if given, which may be residual), y for outputs "same" or
         "both", y8 float8_e4m3fn with y8_scale f32 [rows] for "e4m3" or "both"."""
-        shape, dtype, dev = x.shape, x.dtype, self.device
-        rows, cols = shape
-        assert x.is_cuda and x.stride(1) == 1 and weight.is_cuda and weight.dtype == torch.float32 and weight.is_contiguous() and weight.numel() == cols
-        assert outputs in ("same", "e4m3", "both")
-        total = y = y8 = scale = None
-        rs = ss = cols
-        if residual is not None:
-            assert residual.is_cuda and residual.dtype == dtype and residual.shape == shape and residual.stride(1) == 1
-            total = torch.empty_like(x) if sum_out is None else sum_out          # dense, as x's rows are
-            assert sum_out is None or (total.is_cuda and total.dtype == dtype and total.shape == shape and total.stride(1) == 1)
-            if rows > 1:
-                rs, ss = residual.stride(0), total.stride(0)
-        if outputs != "e4m3":
-            y = torch.empty_like(x)
-        if outputs != "same":
-            y8, scale = torch.empty_like(x, dtype=torch.float8_e4m3fn), torch.empty(rows, dtype=torch.float32, device=dev)
-        self._made(total if sum_out is None else None, y, y8, scale)
-        self._check(self.lib.rh_norm_residual(self.h, x.data_ptr(), x.stride(0) if rows > 1 else cols, None if residual is None else residual.data_ptr(), rs,
-                                              weight.data_ptr(), SEQ_TYPE[dtype], rows, cols, eps, None if total is None else total.data_ptr(), ss,
-                                              None if y is None else y.data_ptr(), None if y8 is None else y8.data_ptr(), None if y8 is None else scale.data_ptr()))
-        return total, y, y8, scale
+        return self._outputs(_seq.norm_residual(self._ctx, x, weight, residual, eps, outputs, sum_out))
 
     def matvec_packed(self, x: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, x_scale: torch.Tensor | None = None,
                       relu: bool = False, out_dtype: torch.dtype | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
         """x [rows, n_in] (float32, bfloat16, or float8_e4m3fn with x_scale f32 [rows]) by weights in 4 bits: w uint8
         [n_out, 16 * ceil(n_in / 32)], w_scale uint8 [n_out, ceil(n_in / 32)] (pack_weights makes them) -> [rows, n_out]."""
-        rows, n_in = x.shape
-        n_out, blocks = w_scale.shape
-        assert x.is_cuda and x.stride(1) == 1 and blocks == (n_in + 31) // 32
-        assert w.is_cuda and w.dtype == torch.uint8 and w.is_contiguous() and w.shape == (n_out, 16 * blocks)
-        assert w_scale.is_cuda and w_scale.dtype == torch.uint8 and w_scale.is_contiguous()
-        assert x_scale is None or (x_scale.is_cuda and x_scale.dtype == torch.float32 and x_scale.is_contiguous() and x_scale.numel() == rows)
-        if out is None:
-            out = torch.empty((rows, n_out), dtype=out_dtype or (torch.float32 if x.dtype == torch.float32 else torch.bfloat16), device=self.device)
-            self._made(out)
-        else:
-            assert out.is_cuda and out.shape == (rows, n_out) and out.stride(1) == 1 and (out_dtype is None or out.dtype == out_dtype)
-        self._check(self.lib.rh_matvec_packed(self.h, x.data_ptr(), SEQ_TYPE[x.dtype], x.stride(0) if rows > 1 else n_in,
-                                              None if x_scale is None else x_scale.data_ptr(), w.data_ptr(), w_scale.data_ptr(), rows, n_out,
-                                              n_in, 1 if relu else 0, out.data_ptr(), SEQ_TYPE[out.dtype], out.stride(0) if rows > 1 else n_out))
-        return out
+        return self._outputs(_seq.matvec_packed(self._ctx, x, w, w_scale, x_scale, relu, out_dtype, out))
 
     def read_counts(self, counts: torch.Tensor):
         out = (C.c_uint32 * 4)()

@@ -678,3 +678,31 @@ def test_empty_batches(rh):
     z = torch.zeros
     assert rh.norm_residual(z((0, 64), device="cuda"), z(64, device="cuda"))[1].shape == (0, 64)
     assert rh.matvec_packed(z((0, 64), device="cuda"), z((8, 32), dtype=torch.uint8, device="cuda"), z((8, 2), dtype=torch.uint8, device="cuda")).shape == (0, 8)
+
+
+def test_tensors_that_do_not_fit_are_refused_in_the_binding(rh):
+    q, cache, table, lengths = _attend_inputs(1, [30, 5], 2, 4, 64, 16, torch.bfloat16, torch.bfloat16)
+    x, w32 = torch.zeros((2, 64), device="cuda"), torch.ones(64, device="cuda")
+    cw, cs = torch.zeros((8, 32), dtype=torch.uint8, device="cuda"), torch.zeros((8, 2), dtype=torch.uint8, device="cuda")
+    i = _i32(np.zeros(2))
+    calls = [
+        lambda: rh.cache_attend(q[:1], cache, table, lengths), lambda: rh.cache_attend(q[..., :32], cache, table, lengths),
+        lambda: rh.cache_attend(q, cache, table.long(), lengths), lambda: rh.cache_attend(q, cache, table, lengths[:1]),
+        lambda: rh.cache_attend(q, cache, table, lengths, out=torch.zeros((2, 8, 64), device="cuda")),
+        lambda: rh.cache_attend(q.cpu(), cache, table, lengths),
+        lambda: KVCache(cache.k, cache.v.float()), lambda: KVCache(cache.k, cache.v[:, :, :1]), lambda: KVCache(cache.k.transpose(2, 3), cache.v.transpose(2, 3)),
+        lambda: KVCache(cache.k, cache.v, i.float(), i.float()),
+        lambda: rh.cache_write(cache, q[:, :2], q[:, :3], i), lambda: rh.cache_write(cache, q[:, :2], q[:, 2:4], i.long()), lambda: rh.cache_write(cache, q[:1, :2], q[:1, 2:4], i),
+        lambda: rh.cache_plan(i, i[:1], table, i, i[:1], 16, 4), lambda: rh.cache_plan(i, i, table[:1], i, i[:1], 16, 4), lambda: rh.cache_plan(i, i, table, i, i, 16, 4),
+        lambda: rh.cache_plan(i, i, table, i, i[:1], 16, 4, new_lengths=i[:1]), lambda: rh.cache_plan(i.float(), i, table, i, i[:1], 16, 4),
+        lambda: rh.norm_residual(x, w32[:5]), lambda: rh.norm_residual(x, w32, x.bfloat16()), lambda: rh.norm_residual(x, w32, x[:1]), lambda: rh.norm_residual(x, w32, outputs="bf16"),
+        lambda: rh.norm_residual(x, w32.double()), lambda: rh.norm_residual(x.t(), w32[:2]), lambda: rh.norm_residual(x, w32, x, sum_out=x.bfloat16()),
+        lambda: rh.matvec_packed(x[:, :32], cw, cs), lambda: rh.matvec_packed(x, cw[:4], cs), lambda: rh.matvec_packed(x, cw, cs, x_scale=w32), lambda: rh.matvec_packed(x, cw.int(), cs),
+        lambda: rh.matvec_packed(x.double(), cw, cs), lambda: rh.matvec_packed(x, cw, cs, out=x), lambda: rh.matvec_packed(x, cw, cs, out=torch.zeros((2, 8), device="cuda"), out_dtype=torch.bfloat16),
+    ]
+    for k, call in enumerate(calls):
+        with pytest.raises(AssertionError):
+            call()
+            print("call", k, "was taken")
+    with pytest.raises(TypeError):
+        rh.cache_attend(q, cache, table, lengths, scale="1")

@@ -94,3 +94,19 @@ for f in (plan, write, attend, norm, matvec):
     assert f() == 4 and L.rh_last_error(ctx)
     rec.rec_reset(); assert f() == 0 and len(names()) == 1
 ''')
+
+
+def test_the_binding_looks_at_its_tensors():
+    """What the library cannot see of a tensor is refused in the binding: where it lies, its type, its shape (no GPU: nothing passes here)."""
+    import pytest
+    import torch
+    from paper_2407_16990_amd import KVCache, binding, load_library
+    load_library()
+    x, w, s = torch.zeros(2, 64), torch.zeros((8, 32), dtype=torch.uint8), torch.zeros((8, 2), dtype=torch.uint8)
+    calls = [lambda: binding._seq.matvec_packed(0, x, w, s, None, False, None, None), lambda: binding._seq.norm_residual(0, x, x[0], None, 1e-6, "same", None),
+             lambda: binding._seq.norm_residual(0, [1.0], x[0], None, 1e-6, "same", None), lambda: binding._seq.matvec_packed(0, x),
+             lambda: binding._seq.cache_plan(0, *[torch.zeros(4, dtype=torch.int32)] * 5, 16, 4, None, None), lambda: binding._seq.cache_write(0, b"", x, x, x),
+             lambda: binding._seq.cache_attend(0, b"no cache", x, x, x, None, 0, None, True), lambda: KVCache(torch.zeros(1, 1, 1, 32), torch.zeros(1, 1, 1, 32))]
+    for call in calls:
+        with pytest.raises(AssertionError):
+            call()
