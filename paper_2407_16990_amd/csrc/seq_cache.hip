@@ -129,11 +129,12 @@ __global__ __launch_bounds__(PLAN_T) void k_seq_plan(plan_args a)
     };
     const int id = blockIdx.x * PLAN_T + t, stride = gridDim.x * PLAN_T;
     const int32_t n_tok = (int32_t)placed[0], n_taken = (int32_t)placed[1], high = (int32_t)top - 1;
-    for (int r = id; r < (int32_t)returned; r += stride) {
+    // pages that come back from the last thread on, pages taken from the middle, slots from the first: mostly no workgroup has to do with two of them
+    for (int r = stride - 1 - id; r < (int32_t)returned; r += stride) {
         const int b = plan_find(s_back, B, r);
         if (height + r < a.n_pages) a.free_pages[height + r] = a.table[(size_t)b * a.max_pages + (r - s_back[b])];
     }
-    for (int i = id; i < n_taken; i += stride) {
+    for (int i = id < stride / 2 ? id + (stride + 1) / 2 : id - stride / 2; i < n_taken; i += stride) {
         const int b = plan_find(s_start, B, i);
         const int have = (int)seq_quot((uint32_t)(s_old[b] + page - 1), a.page);
         a.table[(size_t)b * a.max_pages + have + (i - s_start[b])] = stacked(high - i);
