@@ -11,7 +11,7 @@
  * They take a context of rh.h and follow its conventions: device pointers, caller-owned buffers, all work on the context's
  * stream, arguments checked before any launch, rh_last_error.  They use neither the context's network nor its capacities,
  * and count in no class of rh_profile_read.  Sums, softmax statistics and norms are held in 32 bits.
- * Scratch memory of rh_cache_attend (68 MB on 256 CUs) and a few counters, of rh_cache_plan too, belong to the context: the first call that wants
+ * Scratch memory of rh_cache_attend and rh_matvec_packed (68 MB on 256 CUs) and a few counters, of rh_cache_plan too, belong to the context: the first call that wants
  * them allocates them, no later one allocates or synchronises, so that from then on calls may be captured into graphs.
  */
 #ifndef RH_SEQ_H
@@ -111,6 +111,7 @@ rh_status rh_norm_residual(rh_ctx* ctx, const void* x, int64_t x_stride, const v
  *   share the factor 2^(scale - 127) (255 is not a number).  Codes past n_in do not matter.
  *   x (dev) [n_rows] rows x_stride elements apart, RH_T_F32, RH_T_BF16 or RH_T_E4M3; x_scale (dev) f32 [n_rows]
  *   or NULL for ones.  y (dev): RH_T_F32 or RH_T_BF16, rows y_stride elements apart.
+ * Long rows are cut into slices that workgroups share; sums of one call come in the same order every time.
  */
 rh_status rh_matvec_packed(rh_ctx* ctx, const void* x, int32_t x_type, int64_t x_stride, const float* x_scale,
                            const uint8_t* w, const uint8_t* w_scale, int32_t n_rows, int32_t n_out, int32_t n_in,

@@ -84,8 +84,8 @@ inline seq_div seq_make_div(uint32_t d)
 }
 __device__ __forceinline__ uint32_t seq_quot(uint32_t x, const seq_div& v) { return (__umulhi(x, v.m) + (x & v.one)) >> v.s; }
 
-// Scratch memory: rows of partial results of rh_cache_attend, and as many counters, which are zero between calls (rh_cache_plan takes the
-// first).  A stream cut into n > 1 chunks has more than n - 1 >= n / 2 chunks' tiles, so that of ATTEND_CHUNKS chunks a CU twice as many at most
+// Scratch memory: rows of partial results of rh_cache_attend, or sums of slices of rh_matvec_packed, and as many counters as rows, which are zero between
+// calls (rh_cache_plan takes the first).  A stream cut into n > 1 chunks has more than n - 1 >= n / 2 chunks' tiles, so that of ATTEND_CHUNKS chunks a CU twice as many at most
 // belong to such streams.
 #define ATTEND_CHUNKS 8          // chunks a CU of rh_cache_attend
 #define SEQ_ROWS(ctx) (2 * ATTEND_CHUNKS * (ctx)->n_cu)

@@ -11,20 +11,25 @@
 //               are 1.3e-6 / 3.5e-6 / 4.2e-6 off in norm, 0 / 3e-8 / 7e-8 as bf16 rows.  So it serves bf16 outputs only, whose
 //               rounding is 1.7e-3, and from one whole stretch of 512 terms on, where there is something to gain
 // A workgroup's waves share out its tiles of outputs and the inner index (KS waves a tile, summed in LDS in order), so that few outputs
-// still use every wave.
+// still use every wave; where x is long or the tiles are few, workgroups share the inner index too, and the last of them adds up their sums, in their order.
+// 16 x 16384 x 4096, e4m3 rows: 10.1 us, 3.5 TB/s of weights; 7.0 at a copy's rate, about 2 until the first bytes are there, the rest x.  1 x 1024 x 510,
+// fp32: 4.0, hardly more than an empty launch (2.5) and one way to memory.
 #include "seq_common.h"
 
 struct matvec_args {
     const void* x;
-    const float* x_scale;
     const uint8_t *w, *w_scale;
-    void* y;
-    int64_t x_stride, y_stride;
-    int32_t rows, outs, ins, blocks, relu;
+    int64_t x_stride;
+    int32_t rows, outs, ins, blocks;
     int32_t tiles, ks, tw;       // tiles of outputs; waves a tile; tiles a workgroup at a time
-    int32_t quads, chunk;        // stretches of 512 of the inner index: all, and as many as x lies in LDS for at a time
-    int32_t y_f32;
-    seq_div row_pieces[2];       // 16-byte pieces of a row in LDS: of a whole chunk, of the last
+    int32_t quads, slice, chunk; // stretches of 512 of the inner index: all, a workgroup's, and as many as x lies in LDS for at a time
+    const float* x_scale;
+    void* y;
+    int64_t y_stride;
+    int32_t relu, y_f32;
+    uint64_t* part;              // sums of slices of the inner index [group of rows][tile][R * MT][slice][half][lane]
+    uint32_t* count;             // [group of rows][workgroup of a slice]
+    int32_t slices;
 };
 
 #define MATVEC_WAVES(XT, MT) (MT == 1 && XT != RH_T_F32 ? 16 : 8)       // of a workgroup, one a CU; the others' registers allow eight
@@ -82,7 +87,7 @@ __device__ __forceinline__ bf16x8 matvec_wide_slow(uint32_t c, uint32_t scale)
     return r.all;
 }
 
-template <int XT, int MT, int R>
+template <int XT, int MT, int R, bool SPLIT>
 __global__ __launch_bounds__(64 * MATVEC_WAVES(XT, MT)) void k_seq_matvec(matvec_args a)
 {
     typedef matvec_kind<XT> K;
@@ -91,13 +96,14 @@ __global__ __launch_bounds__(64 * MATVEC_WAVES(XT, MT)) void k_seq_matvec(matvec
     extern __shared__ uint4 s_mem[];
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6, c = lane & 15, j = lane >> 4;
     const int tw = wave / a.ks, ks = wave % a.ks;
+    const int qb = SPLIT ? blockIdx.z * a.slice : 0, qe = SPLIT && qb + a.slice < a.quads ? qb + a.slice : a.quads;       // the workgroup's slice
     const int m0 = blockIdx.y * 16 * MT, M = a.rows - m0 < 16 * MT ? a.rows - m0 : 16 * MT, P = M | 1;
     // x in LDS: pieces of 16 bytes, [part][step][as the lanes of a product read them][row]; an odd number P of rows, or neighbouring
     // pieces of a row would be written to the same banks (16 x 4096 x 4096, bf16 rows: 8.4 -> 6.9 us)
     const int part_pieces = a.chunk * 4 * PER_STEP * P;
     u32x4* xs = (u32x4*)s_mem;
     // the waves' sums [wave][R * MT][lane]: behind x, or in its place where x does not lie here as a whole
-    f32x4* s_sum = (f32x4*)(a.chunk < a.quads ? xs : xs + PARTS * part_pieces);
+    f32x4* s_sum = (f32x4*)(a.chunk < a.slice ? xs : xs + PARTS * part_pieces);
 
     constexpr int W = PIECE * sizeof(T) / 4;                 // words of a piece in memory
     auto put = [&](int m, int p, const uint32_t* v) {        // piece p of row m
@@ -130,7 +136,10 @@ __global__ __launch_bounds__(64 * MATVEC_WAVES(XT, MT)) void k_seq_matvec(matvec
     };
     auto stage = [&](int q0, int nq) {
         const int per_row = nq * 4 * PER_STEP, all = per_row * M;                          // pieces: of a row, of all
-        const seq_div& div = a.row_pieces[nq < a.chunk];
+        // i / per_row by a product: (i + 1/2) / per_row is at least 1 / (2 per_row) away from a whole number, and the product's error, below
+        // 2^-21 of it, stays below that, since i < 2^14 (what fits the LDS)
+        const float inverse = __builtin_amdgcn_rcpf((float)per_row);
+        auto row = [&](int i) { return (int)(((float)i + 0.5f) * inverse); };
         if ((q0 + nq) * 512 <= a.ins) {
             constexpr int AHEAD = 4;                         // pieces of a thread in flight
             for (int first = t; first < all; first += AHEAD * blockDim.x) {
@@ -140,7 +149,7 @@ __global__ __launch_bounds__(64 * MATVEC_WAVES(XT, MT)) void k_seq_matvec(matvec
                 for (int k = 0; k < AHEAD; ++k) {            // behind the last: the last again
                     int i = first + k * (int)blockDim.x;
                     i = i < all ? i : all - 1;
-                    m[k] = (int)seq_quot((uint32_t)i, div); p[k] = i - m[k] * per_row;
+                    m[k] = row(i); p[k] = i - m[k] * per_row;
                     get((const T*)a.x + (m0 + m[k]) * a.x_stride + q0 * 512 + p[k] * PIECE, v[k]);
                 }
 #pragma unroll
@@ -148,7 +157,7 @@ __global__ __launch_bounds__(64 * MATVEC_WAVES(XT, MT)) void k_seq_matvec(matvec
             }
         } else
             for (int i = t; i < all; i += blockDim.x) {      // rows that end in here: zeros behind
-                const int m = (int)seq_quot((uint32_t)i, div), p = i - m * per_row, e = q0 * 512 + p * PIECE, n = a.ins - e;
+                const int m = row(i), p = i - m * per_row, e = q0 * 512 + p * PIECE, n = a.ins - e;
                 const T* from = (const T*)a.x + (m0 + m) * a.x_stride + e;
                 uint32_t v[W] = {};
                 if (n >= PIECE) get(from, v);
@@ -166,7 +175,7 @@ __global__ __launch_bounds__(64 * MATVEC_WAVES(XT, MT)) void k_seq_matvec(matvec
     // ---- a wave's weights: tile by tile of outputs, of each its share of the stretches of every chunk
     struct place { int tile, q0, q, end; };                  // q0: the chunk's first stretch; q, end: of the wave's share, in the chunk
     auto share = [&](place& p) {
-        const int n = a.quads - p.q0 < a.chunk ? a.quads - p.q0 : a.chunk, each = (n + a.ks - 1) / a.ks;
+        const int n = qe - p.q0 < a.chunk ? qe - p.q0 : a.chunk, each = (n + a.ks - 1) / a.ks;
         p.q = ks * each;
         p.end = p.q + each < n ? p.q + each : n;
     };
@@ -176,7 +185,7 @@ __global__ __launch_bounds__(64 * MATVEC_WAVES(XT, MT)) void k_seq_matvec(matvec
         ++p.q;
         while (p.q >= p.end) {
             p.q0 += a.chunk;
-            if (p.q0 >= a.quads) { p.q0 = 0; p.tile += tile_step; }
+            if (p.q0 >= qe) { p.q0 = qb; p.tile += tile_step; }
             if (p.tile >= a.tiles) return false;
             share(p);
         }
@@ -284,33 +293,32 @@ __global__ __launch_bounds__(64 * MATVEC_WAVES(XT, MT)) void k_seq_matvec(matvec
         }
     };
 
-    auto write = [&](int tile) {
+    auto write = [&](int tile, int r, int i, f32x4 v) {
+        const int m = 16 * i + c, n = (tile * R + r) * 16 + 4 * j;
+        if (m >= M || n >= a.outs) return;
+        if (a.x_scale) v *= a.x_scale[m0 + m];
+        if (a.relu) {
 #pragma unroll
-        for (int r = 0; r < R; ++r)
-#pragma unroll
-            for (int i = 0; i < MT; ++i) {
-                const int m = 16 * i + c, n = (tile * R + r) * 16 + 4 * j;
-                if (m >= M || n >= a.outs) continue;
-                f32x4 v = acc[r][i];
-                if (a.x_scale) v *= a.x_scale[m0 + m];
-                if (a.relu) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] = v[e] < 0.f ? 0.f : v[e];
-                }
-                const int64_t at = (m0 + m) * a.y_stride + n;
-                if (a.y_f32) {
-                    float* o = (float*)a.y + at;
-                    if (n + 4 <= a.outs) seq_store(o, v);
-                    else for (int e = 0; n + e < a.outs; ++e) o[e] = v[e];
-                } else {
-                    __bf16* o = (__bf16*)a.y + at;
-                    if (n + 4 <= a.outs) seq_store(o, make_uint2(seq_pack_bf16(v[0], v[1]), seq_pack_bf16(v[2], v[3])));
-                    else for (int e = 0; n + e < a.outs; ++e) o[e] = (__bf16)v[e];
-                }
-            }
+            for (int e = 0; e < 4; ++e) v[e] = v[e] < 0.f ? 0.f : v[e];
+        }
+        const int64_t at = (m0 + m) * a.y_stride + n;
+        if (a.y_f32) {
+            float* o = (float*)a.y + at;
+            if (n + 4 <= a.outs) seq_store(o, v);
+            else for (int e = 0; n + e < a.outs; ++e) o[e] = v[e];
+        } else {
+            __bf16* o = (__bf16*)a.y + at;
+            if (n + 4 <= a.outs) seq_store(o, make_uint2(seq_pack_bf16(v[0], v[1]), seq_pack_bf16(v[2], v[3])));
+            else for (int e = 0; n + e < a.outs; ++e) o[e] = (__bf16)v[e];
+        }
     };
 
-    place at = {(int)blockIdx.x * a.tw + tw, 0, 0, 0};
+    struct two { uint64_t u[2]; };
+    auto part = [&](int tile, int z, int r, int i) {
+        return a.part + (((((size_t)blockIdx.y * a.tiles + tile) * R + r) * MT + i) * a.slices + z) * 128 + lane;
+    };
+
+    place at = {(int)blockIdx.x * a.tw + tw, qb, 0, 0};
     weights now, next;
     const bool idle = tw >= a.tw;                            // waves that only help to lay x out
     bool have = !idle && at.tile < a.tiles;
@@ -326,10 +334,10 @@ __global__ __launch_bounds__(64 * MATVEC_WAVES(XT, MT)) void k_seq_matvec(matvec
         for (int r = 0; r < R; ++r)
 #pragma unroll
             for (int i = 0; i < MT; ++i) acc[r][i] = f32x4{0.f, 0.f, 0.f, 0.f};
-        for (int q0 = 0; q0 < a.quads; q0 += a.chunk) {
+        for (int q0 = qb; q0 < qe; q0 += a.chunk) {
             if (staged != q0) {
                 if (staged >= 0) __syncthreads();
-                stage(q0, a.quads - q0 < a.chunk ? a.quads - q0 : a.chunk);
+                stage(q0, qe - q0 < a.chunk ? qe - q0 : a.chunk);
                 __syncthreads();
                 staged = q0;
             }
@@ -357,10 +365,69 @@ __global__ __launch_bounds__(64 * MATVEC_WAVES(XT, MT)) void k_seq_matvec(matvec
 #pragma unroll
                         for (int i = 0; i < MT; ++i) acc[r][i] += s_sum[((wave + k) * R * MT + r * MT + i) * 64 + lane];
             }
-            if (a.chunk < a.quads) staged = a.quads;         // no chunk: the sums lie there
+            if (a.chunk < a.slice) staged = a.quads;         // no chunk: the sums lie there
         }
-        if (!ks && !idle && tile < a.tiles) write(tile);
+        if (ks || idle || tile >= a.tiles) continue;
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+                if constexpr (!SPLIT) write(tile, r, i, acc[r][i]);
+                else if (16 * i + c < M) {
+                    const two v = __builtin_bit_cast(two, acc[r][i]);
+                    uint64_t* p = part(tile, blockIdx.z, r, i);
+                    __hip_atomic_store(p, v.u[0], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                    __hip_atomic_store(p + 64, v.u[1], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                }
+            }
     }
+    if constexpr (!SPLIT) return;
+    // ---- the slices' sums: the workgroup that comes last with its tiles adds them up, in the slices' order.  Slices run on several XCDs: sums are stored
+    // through and loaded past the L2, and acknowledged before they are counted.
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    uint32_t* s_last = (uint32_t*)s_mem;
+    if (t == 0) {
+        uint32_t* count = a.count + blockIdx.y * gridDim.x + blockIdx.x;
+        const bool last = __hip_atomic_fetch_add(count, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)a.slices - 1;
+        if (last) __hip_atomic_store(count, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        *s_last = last;
+    }
+    __syncthreads();
+    if (!*s_last) return;
+    const int rounds = (a.tiles - (int)blockIdx.x * a.tw + tile_step - 1) / tile_step, vectors = rounds * a.tw * R * MT;
+    auto join = [&](auto ahead) __attribute__((always_inline)) {
+        constexpr int Z = decltype(ahead)::value, N = 16 / Z;                  // a wave loads Z slices of N vectors at a time
+        for (int n0 = wave * N; n0 < vectors; n0 += (blockDim.x >> 6) * N) {
+            f32x4 sum[N] = {};
+            for (int z = 0; z < a.slices; z += Z) {
+                two v[N][Z];
+#pragma unroll
+                for (int q = 0; q < N; ++q) {
+                    const int n = n0 + q, nth = n / (R * MT);
+                    int tile = blockIdx.x * a.tw + nth / a.tw * tile_step + nth % a.tw;
+                    tile = tile < a.tiles ? tile : a.tiles - 1;
+#pragma unroll
+                    for (int k = 0; k < Z; ++k) {
+                        const uint64_t* p = part(tile, z + k < a.slices ? z + k : z, n / MT % R, n % MT);
+                        v[q][k].u[0] = __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                        v[q][k].u[1] = __hip_atomic_load(p + 64, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                    }
+                }
+#pragma unroll
+                for (int q = 0; q < N; ++q)
+#pragma unroll
+                    for (int k = 0; k < Z; ++k)
+                        if (z + k < a.slices) sum[q] += __builtin_bit_cast(f32x4, v[q][k]);
+            }
+#pragma unroll
+            for (int q = 0; q < N; ++q) {
+                const int n = n0 + q, nth = n / (R * MT), tile = blockIdx.x * a.tw + nth / a.tw * tile_step + nth % a.tw;
+                if (n < vectors && tile < a.tiles) write(tile, n / MT % R, n % MT, sum[q]);
+            }
+        }
+    };
+    if (a.slices <= 4) join(seq_const<4>()); else if (a.slices <= 8) join(seq_const<8>()); else join(seq_const<16>());
 }
 
 template <int XT, int MT, int R>
@@ -369,33 +436,66 @@ static hipError_t launch_matvec(rh_ctx* ctx, matvec_args a)
     typedef matvec_kind<XT> K;
     static bool attr_done[RH_MAX_DEVICES] = {};              // the attribute is per device
     if (!attr_done[ctx->device]) {
-        const hipError_t e = hipFuncSetAttribute((const void*)k_seq_matvec<XT, MT, R>, hipFuncAttributeMaxDynamicSharedMemorySize, MATVEC_LDS);
-        if (e != hipSuccess) return e;
+        for (const void* f : {(const void*)k_seq_matvec<XT, MT, R, false>, (const void*)k_seq_matvec<XT, MT, R, true>}) {
+            const hipError_t e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, MATVEC_LDS);
+            if (e != hipSuccess) return e;
+        }
         attr_done[ctx->device] = true;
     }
     const int M = a.rows < 16 * MT ? a.rows : 16 * MT, quad = K::PARTS * 512 / K::PIECE * 16 * (M | 1);       // bytes of x in LDS, of a stretch
-    constexpr int WAVES = MATVEC_WAVES(XT, MT), sums = WAVES * R * MT * 64 * (int)sizeof(f32x4);
+    constexpr int WAVES = MATVEC_WAVES(XT, MT), SUMS = WAVES * R * MT * 64 * (int)sizeof(f32x4);
+    const int gy = (a.rows + 16 * MT - 1) / (16 * MT);
     a.quads = (a.ins + 511) / 512;
-    const bool whole = a.quads * (int64_t)quad + sums <= MATVEC_LDS;
-    a.chunk = whole ? a.quads : MATVEC_LDS / quad < a.quads - 1 ? MATVEC_LDS / quad : a.quads - 1;
-    a.chunk = a.chunk < 1 ? 1 : a.chunk;
     a.tiles = (a.outs + 16 * R - 1) / (16 * R);
-    a.row_pieces[0] = seq_make_div(a.chunk * (512 / K::PIECE));
-    a.row_pieces[1] = seq_make_div(a.quads % a.chunk ? a.quads % a.chunk * (512 / K::PIECE) : 1);
     // One workgroup a CU, so that x is laid out there once.  A tile a workgroup (several where there are more tiles than that), the other
     // waves share its inner index.
-    const int wgs = ctx->n_cu, each = (a.tiles + wgs - 1) / wgs;
-    a.tw = 1;
-    while (a.tw < each && a.tw < WAVES) a.tw *= 2;
-    a.ks = 1;
-    while (a.ks * a.tw < WAVES && a.ks < a.chunk) a.ks *= 2;
-    const int groups = (a.tiles + a.tw - 1) / a.tw;
-    // and as many more as have eight pieces of x each to lay out
+    int groups = 0;
+    bool whole = false;
+    auto cut = [&](int slices) {                             // the launch with so many slices; us that depend on their number
+        a.slice = (a.quads + slices - 1) / slices;
+        a.slices = (a.quads + a.slice - 1) / a.slice;
+        whole = a.slice * (int64_t)quad + SUMS <= MATVEC_LDS;
+        a.chunk = whole ? a.slice : MATVEC_LDS / quad < a.slice - 1 ? MATVEC_LDS / quad : a.slice - 1;
+        a.chunk = a.chunk < 1 ? 1 : a.chunk;
+        int wgs = ctx->n_cu / (gy * a.slices);
+        wgs = a.slices == 1 && wgs < 16 ? 16 : wgs;          // many groups of rows: few workgroups more than CUs would leave most of them idle at the end
+        const int each = (a.tiles + wgs - 1) / wgs;
+        a.tw = 1;
+        while (a.tw < each && a.tw < WAVES) a.tw *= 2;
+        a.ks = 1;
+        while (a.ks * a.tw < WAVES && a.ks < a.chunk) a.ks *= 2;
+        groups = (a.tiles + a.tw - 1) / a.tw;
+        groups = groups < wgs ? groups : wgs;
+        const int rounds = (a.tiles + groups * a.tw - 1) / (groups * a.tw), full = a.slice / a.chunk, rest = a.slice % a.chunk;
+        const int depth = rounds * (full * ((a.chunk + a.ks - 1) / a.ks) + (rest + a.ks - 1) / a.ks);          // stretches a wave goes through
+        const float laid = (float)(K::PARTS * 512 * (16 / K::PIECE)) * M * a.slice * (whole ? 1 : rounds), read = (float)rounds * a.tw * R * 16 * 272 * a.slice;
+        const float join = a.slices == 1 ? 0.f : (a.slices > 8 ? 3.9f : 2.9f) + 1.1e-6f * a.slices * gy * a.tiles * (R * MT * 1024.f);
+        return 25e-6f * laid + 14e-6f * read + 1.7f * depth + join;
+    };
+    // The inner index may be cut into slices too, a workgroup each, whose sums are joined in the same launch: where x is long, or the tiles are
+    // few, a workgroup's slice of x takes less than the whole of it.  A line through times of 72 shapes (1 to 64 rows, 64 to 4096 outputs, 1024 to
+    // 16384 inputs, every type of row) at nine numbers of slices, 10 % off in the mean, tells when: 25 us a MB of x laid out in LDS, 14 a MB of weights
+    // that a workgroup reads, 1.7 a stretch that a wave goes through one after another, 2.9 for the join, 1 more for a second batch of loads there, 1.1 a MB
+    // of sums.  What it picks is 1 % slower than the best of the nine in the mean, 11 % at most.  fp32 rows, 16 x 256 x 16384: 64.6 us as a
+    // whole, 12.9 in 16 slices; 1 x 4096 x 1024 5.6 and 8.3 in two.
+    int best = 1;
+    if (a.quads > 1) {
+        float least = cut(1);
+        for (int slices : {2, 4, 6, 8, 11, 16, 22, 32}) {
+            if (slices > a.quads || gy * slices > ctx->n_cu || (size_t)slices * gy * a.tiles * (R * MT * 1024) > (size_t)SEQ_ROWS(ctx) * SEQ_ROW_BYTES(RH_SEQ_MAX_DIM)) break;
+            const float us = cut(slices);
+            if (us < least) { least = us; best = slices; }
+        }
+    }
+    cut(best);
+    // waves, and as many more as have eight pieces of x each to lay out
     const int64_t pieces = (int64_t)a.chunk * (512 / K::PIECE) * M;
     int waves = a.tw * a.ks;
     while (waves < WAVES && (int64_t)waves * 64 * 8 <= pieces) ++waves;
-    hipLaunchKernelGGL((k_seq_matvec<XT, MT, R>), dim3(groups < wgs ? groups : wgs, (a.rows + 16 * MT - 1) / (16 * MT)), dim3(64 * waves),
-                       whole ? (size_t)a.quads * quad + (a.ks > 1 ? sums : 0) : MATVEC_LDS, ctx->stream, a);
+    const dim3 grid(groups, gy, a.slices), block(64 * waves);
+    const size_t lds = whole ? (size_t)a.slice * quad + (a.ks > 1 ? SUMS : 0) : MATVEC_LDS;
+    if (a.slices > 1) hipLaunchKernelGGL((k_seq_matvec<XT, MT, R, true>), grid, block, lds, ctx->stream, a);
+    else hipLaunchKernelGGL((k_seq_matvec<XT, MT, R, false>), grid, block, lds, ctx->stream, a);
     return hipGetLastError();
 }
 
@@ -416,6 +516,10 @@ extern "C" rh_status rh_matvec_packed(rh_ctx* ctx, const void* x, int32_t x_type
     matvec_args a = {};
     a.x = x; a.x_scale = x_scale; a.w = w; a.w_scale = w_scale; a.y = y; a.x_stride = x_stride; a.y_stride = y_stride;
     a.rows = n_rows; a.outs = n_out; a.ins = n_in; a.blocks = (n_in + 31) / 32; a.relu = relu; a.y_f32 = y_type == RH_T_F32;
+    rh_status ws = seq_counters(ctx);
+    if (ws == RH_OK) ws = seq_scratch(ctx);
+    if (ws != RH_OK) return ws;
+    a.part = (uint64_t*)ctx->seq_ws; a.count = ctx->seq_cnt;
     // Rows a pass: more read the weights fewer times; what x takes of the LDS, and sums of registers, bounds them.
     hipError_t e;
     if (x_type == RH_T_F32) e = launch_matvec<RH_T_F32, 1, 1>(ctx, a);

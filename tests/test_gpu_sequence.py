@@ -505,6 +505,67 @@ def test_matvec(rh, dtype, rows, n_out, n_in):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,n_out,n_in", [(1, 200, 16000), (16, 7, 4096), (16, 300, 16384), (13, 260, 15361), (31, 500, 7777), (40, 1000, 8000), (64, 129, 12288), (64, 2100, 5000), (200, 33, 9000),
+                                             (1, 16, 40000), (64, 3000, 16384)])
+def test_matvec_long_rows(rh, dtype, rows, n_out, n_in):
+    """Long rows, whose inner index several workgroups share: what they add up, and that it is the same every time, also between calls of
+    other shapes that use the same scratch memory."""
+    g = torch.Generator(device="cuda").manual_seed(rows + n_out + n_in)
+    w, sc = _weights(g, n_out, n_in)
+    x = _rows(g, rows, n_in, dtype, gap=rows % 2 * 3)
+    xs = torch.rand(rows, generator=g, device="cuda") * 0.1 if n_out % 2 else None
+    w2, sc2 = _weights(g, 400, 16384)
+    x2 = _rows(g, 16, 16384, torch.float32)
+    other = rh.matvec_packed(x2, w2, sc2)
+    for relu, out in ((False, torch.float32), (True, torch.bfloat16)):
+        y = _check_matvec(rh, x, w, sc, xs, relu, out)
+        for _ in range(3):
+            assert torch.equal(rh.matvec_packed(x2, w2, sc2), other)
+            assert torch.equal(rh.matvec_packed(x, w, sc, x_scale=xs, relu=relu, out_dtype=out), y)
+
+
+def test_matvec_long_rows_hold_what_is_not_finite(rh):
+    """An infinity or NaN of a row stays in that row's outputs, wherever along the row it lies."""
+    g = torch.Generator(device="cuda").manual_seed(8)
+    w, sc = _weights(g, 70, 16384)
+    w |= 0x11                                                      # no weight is zero
+    for dtype in TYPES:
+        x = _rows(g, 16, 16384, dtype).clone()
+        want = rh.matvec_packed(x, w, sc, out_dtype=torch.float32)
+        for at in (0, 511, 8000, 16383):
+            bad = x.clone()
+            bad[5, at] = float("nan")
+            y = rh.matvec_packed(bad, w, sc, out_dtype=torch.float32)
+            assert bool(y[5].isnan().all()), at
+            y[5] = want[5]
+            assert torch.equal(y, want)
+
+
+def test_matvec_long_rows_in_a_graph(rh):
+    g = torch.Generator(device="cuda").manual_seed(12)
+    w, sc = _weights(g, 300, 16384)
+    x = torch.zeros((16, 16384), device="cuda")
+    rh.matvec_packed(x, w, sc)                                     # the scratch memory is there
+    torch.cuda.synchronize()
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    rh.lib.rh_set_stream(rh.h, side.cuda_stream)
+    rh._stream = side
+    try:
+        with torch.cuda.graph(graph, stream=side):
+            got = rh.matvec_packed(x, w, sc)
+    finally:
+        rh._stream = torch.cuda.current_stream()
+        rh.lib.rh_set_stream(rh.h, rh._stream.cuda_stream)
+    for i in range(5):
+        x.copy_(torch.randn(x.shape, generator=g, device="cuda"))
+        graph.replay()
+        torch.cuda.synchronize()
+        want = rh.matvec_packed(x, w, sc)
+        torch.cuda.synchronize()
+        assert torch.equal(got, want), i
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 def test_matvec_every_code_and_scale(rh, dtype):
     """One weight a row of outputs: every code at every scale byte (255 is not a number), an input of one."""
     w = torch.zeros((4096, 16), dtype=torch.uint8, device="cuda")
