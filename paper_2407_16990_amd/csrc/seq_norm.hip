@@ -3,6 +3,8 @@
 // Bound by memory: x and the residual are read once, the sum, y and its 8-bit form written once.  A row stays in the
 // registers of the waves that own it: the mean square, and then the largest |y|, are sums and maxima over them.
 // A row belongs to one wave where it is short, so that a workgroup of four waves needs no barrier.
+// 14720 x 4095 of fp32, all outputs: 186 us, 5.5 TB/s; of bf16 127, 4.3 TB/s (rows at odd addresses; 4092: 108, 5.0 TB/s); 8 x 1024 of
+// bf16 4.3, hardly more than an empty launch and two ways to memory.
 #include "seq_common.h"
 
 struct norm_args {
@@ -16,40 +18,59 @@ struct norm_args {
     float eps;
 };
 
-// E elements (16 bytes) from a row that may start at any element; `n` of them exist.
+// 16 bytes of a row of `cols` elements from element c on, of which the row may have fewer: all lanes load whole pieces that lie in the
+// row, the last ones from further ahead, and norm_place moves those to their place, with zeros behind.  (A branch for them, element by
+// element, was a way to memory of its own: 14720 x 4092 of bf16 126 us, now 108.)
 template <typename T, int E>
-__device__ __forceinline__ void norm_load(const T* p, int n, float (&v)[E])
+__device__ __forceinline__ u32x4 norm_load(const T* row, int c, int cols)
 {
-    if (n >= E) {
-        if constexpr (sizeof(T) == 2) {
-            const uint4 u = seq_load<uint4>(p);
-            const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+    if (cols >= E) return seq_load<u32x4>(row + (c < cols - E ? c : cols - E));
+    u32x4 w = {0, 0, 0, 0};                                  // a row shorter than a piece
 #pragma unroll
-            for (int i = 0; i < 4; ++i) { v[2 * i] = seq_bf16_lo(w[i]); v[2 * i + 1] = seq_bf16_hi(w[i]); }
-        } else {
-            const f32x4 a = seq_load<f32x4>(p);
+    for (int i = 0; i < E; ++i)
+        if (c + i < cols) w[i * (int)sizeof(T) / 4] |= sizeof(T) == 4 ? *(const uint32_t*)(row + c + i) : (uint32_t)*(const uint16_t*)(row + c + i) << (16 * (i & 1));
+    return w;
+}
+template <typename T, int E>
+__device__ __forceinline__ void norm_place(u32x4 w, int c, int cols, float (&v)[E])
+{
+    const int s = cols >= E && c > cols - E ? c - (cols - E) : 0;            // elements that w is ahead by
+    if (__any(s)) {
+        constexpr int W = 4 / sizeof(T);                     // elements of a word
+        if (s & 2 * W) w = u32x4{w[2], w[3], 0, 0};
+        if (s & W) w = u32x4{w[1], w[2], w[3], 0};
+        if (W == 2 && (s & 1))
+            w = u32x4{w[0] >> 16 | w[1] << 16, w[1] >> 16 | w[2] << 16, w[2] >> 16 | w[3] << 16, w[3] >> 16};
+        if (s >= E) w = u32x4{0, 0, 0, 0};
+    }
+    if constexpr (sizeof(T) == 2) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = a[i];
-        }
+        for (int i = 0; i < 4; ++i) { v[2 * i] = seq_bf16_lo(w[i]); v[2 * i + 1] = seq_bf16_hi(w[i]); }
     } else {
 #pragma unroll
-        for (int i = 0; i < E; ++i) v[i] = i < n ? seq_to_f32(p[i]) : 0.f;
+        for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(w[i]);
     }
+}
+
+// the first `bytes` of w, or all 16; whole elements of B bytes
+template <int B>
+__device__ __forceinline__ void norm_put(uint8_t* p, int bytes, u32x4 w)
+{
+    if (bytes >= 16) { seq_store(p, w); return; }
+    if (bytes & 8) { seq_store(p, make_uint2(w[0], w[1])); p += 8; w = u32x4{w[2], w[3], 0, 0}; }
+    if (bytes & 4) { seq_store(p, w[0]); p += 4; w[0] = w[1]; }
+    if (B < 4 && (bytes & 2)) { seq_store(p, (uint16_t)w[0]); p += 2; w[0] >>= 16; }
+    if (B < 2 && (bytes & 1)) *p = (uint8_t)w[0];
 }
 
 template <typename T, int E>
 __device__ __forceinline__ void norm_store(T* p, int n, const float (&v)[E])
 {
-    if (n >= E) {
-        if constexpr (sizeof(T) == 2) {
-            uint4 u;
-            u.x = seq_pack_bf16(v[0], v[1]); u.y = seq_pack_bf16(v[2], v[3]); u.z = seq_pack_bf16(v[4], v[5]); u.w = seq_pack_bf16(v[6], v[7]);
-            seq_store(p, u);
-        } else seq_store(p, f32x4{v[0], v[1], v[2], v[3]});
-    } else {
+    u32x4 w;
 #pragma unroll
-        for (int i = 0; i < E; ++i) if (i < n) p[i] = (T)v[i];
-    }
+    for (int i = 0; i < 4; ++i)
+        if constexpr (sizeof(T) == 2) w[i] = seq_pack_bf16(v[2 * i], v[2 * i + 1]); else w[i] = __float_as_uint(v[i]);
+    norm_put<(int)sizeof(T)>((uint8_t*)p, n * (int)sizeof(T), w);
 }
 
 // The sum (MAX: the largest, a NaN staying) of a value of every thread of a row's WAVES waves.
@@ -71,9 +92,9 @@ __device__ __forceinline__ float norm_over(float v, float* s_part)
 }
 
 template <typename T, int WAVES, int ITEMS>
-__global__ __launch_bounds__(WAVES > 4 ? WAVES * 64 : 256) void k_seq_norm(norm_args a)
+__global__ __launch_bounds__(WAVES > 1 ? WAVES * 64 : 256) void k_seq_norm(norm_args a)
 {
-    constexpr int E = 16 / sizeof(T), NT = WAVES * 64, PER = WAVES > 4 ? 1 : 4 / WAVES;       // threads a row, rows a workgroup
+    constexpr int E = 16 / sizeof(T), NT = WAVES * 64, PER = WAVES > 1 ? 1 : 4;       // threads a row, rows a workgroup
     __shared__ float s_part[WAVES > 1 ? WAVES * PER : 1];
     const int t = threadIdx.x % NT, sub = threadIdx.x / NT;
     const int row = blockIdx.x * PER + sub;
@@ -81,19 +102,20 @@ __global__ __launch_bounds__(WAVES > 4 ? WAVES * 64 : 256) void k_seq_norm(norm_
     const T* x = (const T*)a.x + row * a.x_stride;
     const T* r = (const T*)a.residual + row * a.residual_stride;
     float v[ITEMS][E], square = 0.f;
+    u32x4 in[ITEMS], add[ITEMS];
 #pragma unroll
-    for (int i = 0; i < ITEMS; ++i) {
-        const int c = (t + i * NT) * E, n = a.cols - c;
-        if (n > 0) norm_load<T, E>(x + c, n, v[i]);
-        else { for (int e = 0; e < E; ++e) v[i][e] = 0.f; }
+    for (int i = 0; i < ITEMS; ++i) in[i] = norm_load<T, E>(x, (t + i * NT) * E, a.cols);
+    if (a.residual) {
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) add[i] = norm_load<T, E>(r, (t + i * NT) * E, a.cols);
     }
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) norm_place<T, E>(in[i], (t + i * NT) * E, a.cols, v[i]);
     if (a.residual) {
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {
-            const int c = (t + i * NT) * E, n = a.cols - c;
-            if (n <= 0) continue;
             float u[E];
-            norm_load<T, E>(r + c, n, u);
+            norm_place<T, E>(add[i], (t + i * NT) * E, a.cols, u);
 #pragma unroll
             for (int e = 0; e < E; ++e) v[i][e] += u[e];
         }
@@ -114,25 +136,33 @@ __global__ __launch_bounds__(WAVES > 4 ? WAVES * 64 : 256) void k_seq_norm(norm_
     if (!a.y && !a.y8) return;
     const float scale = 1.f / sqrtf(square / (float)a.cols + a.eps);
     float most = 0.f;
+    constexpr int AHEAD = ITEMS < 4 ? ITEMS : 4;             // items whose weights are in flight
 #pragma unroll
-    for (int i = 0; i < ITEMS; ++i) {
-        const int c = (t + i * NT) * E, n = a.cols - c;
-        if (n <= 0) continue;
-        float w[E];
+    for (int i0 = 0; i0 < ITEMS; i0 += AHEAD) {
+        u32x4 weight[AHEAD][E / 4];
 #pragma unroll
-        for (int e = 0; e < E; e += 4) {
-            float u[4];
-            norm_load<float, 4>(a.weight + c + e, n - e, u);
+        for (int i = 0; i < AHEAD; ++i)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) w[e + k] = u[k];
+            for (int e = 0; e < E; e += 4) weight[i][e / 4] = norm_load<float, 4>(a.weight, (t + (i0 + i) * NT) * E + e, a.cols);
+#pragma unroll
+        for (int i = i0; i < i0 + AHEAD; ++i) {
+            const int c = (t + i * NT) * E, n = a.cols - c;
+            float w[E];
+#pragma unroll
+            for (int e = 0; e < E; e += 4) {
+                float u[4];
+                norm_place<float, 4>(weight[i - i0][e / 4], c + e, a.cols, u);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) w[e + k] = u[k];
+            }
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                v[i][e] = v[i][e] * scale * w[e];
+                const float m = fabsf(v[i][e]);
+                most = m != m || m > most ? m : most;
+            }
+            if (a.y && n > 0) norm_store<T, E>((T*)a.y + (int64_t)row * a.cols + c, n, v[i]);
         }
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-            v[i][e] = v[i][e] * scale * w[e];
-            const float m = fabsf(v[i][e]);
-            most = m != m || m > most ? m : most;
-        }
-        if (a.y) norm_store<T, E>((T*)a.y + (int64_t)row * a.cols + c, n, v[i]);
     }
     if (!a.y8) return;
     most = norm_over<WAVES, true>(most, s_part);
@@ -144,15 +174,12 @@ __global__ __launch_bounds__(WAVES > 4 ? WAVES * 64 : 256) void k_seq_norm(norm_
         const int c = (t + i * NT) * E, n = a.cols - c;
         if (n <= 0) continue;
         uint8_t* o = a.y8 + (int64_t)row * a.cols + c;
-        uint32_t q[E / 4];
+        u32x4 q = {0, 0, 0, 0};
 #pragma unroll
         for (int e = 0; e < E; e += 4) q[e / 4] = seq_pack_e4m3(v[i][e] * inv, v[i][e + 1] * inv, v[i][e + 2] * inv, v[i][e + 3] * inv);
-        if (n >= E) {
-            if constexpr (E == 8) seq_store(o, make_uint2(q[0], q[1])); else seq_store(o, q[0]);
-        } else {
-#pragma unroll
-            for (int e = 0; e < E; ++e) if (e < n) o[e] = (uint8_t)(q[e / 4] >> (8 * (e & 3)));
-        }
+        if (n < E) norm_put<1>(o, n, q);
+        else if constexpr (E == 8) seq_store(o, make_uint2(q[0], q[1]));
+        else seq_store(o, q[0]);
     }
 }
 
@@ -161,16 +188,18 @@ static void launch_norm(hipStream_t s, const norm_args& a)
 {
     constexpr int E = 16 / sizeof(T);
     const int pieces = (a.cols + E - 1) / E;                 // of 16 bytes, one a thread and item
-#define N(WAVES, ITEMS) hipLaunchKernelGGL((k_seq_norm<T, WAVES, ITEMS>), dim3(WAVES > 4 ? a.rows : (a.rows + 4 / WAVES - 1) / (4 / WAVES)), \
-                                           dim3(WAVES > 4 ? WAVES * 64 : 256), 0, s, a)
+#define N(WAVES, ITEMS) hipLaunchKernelGGL((k_seq_norm<T, WAVES, ITEMS>), dim3(WAVES > 1 ? a.rows : (a.rows + 3) / 4), \
+                                           dim3(WAVES > 1 ? WAVES * 64 : 256), 0, s, a)
+    // Two pieces a thread while a workgroup's waves last.  8 rows of 1800 in bf16: 4.7 us, with four a thread in one wave 6.3, with one a thread 4.4; 14720 of 1024 in fp32
+    // 43.5, 43.5, 47.5; 1000 of 4095 in fp32 13.5, 13.6, 16.7.  A single row of 8000 in bf16 4.9, 5.8, 5.3.
     if (pieces <= 64) N(1, 1);
     else if (pieces <= 128) N(1, 2);
-    else if (pieces <= 256) N(1, 4);
+    else if (pieces <= 256) N(2, 2);
     else if (pieces <= 512) N(4, 2);
-    else if (pieces <= 1024) N(4, 4);
-    else if (pieces <= 2048) N(16, 2);
+    else if (pieces <= 1024) N(8, 2);
+    else if (pieces <= 2048) N(8, 4);
     else if (pieces <= 4096) N(16, 4);
-    else N(16, 8);
+    else if constexpr (E == 4) N(16, 8);                     // of bf16 none is that long
 #undef N
 }
 

@@ -449,6 +449,26 @@ def test_norm_strided_rows_and_in_place(rh, dtype):
     assert torch.equal(other[:, 501:], keep[:, 501:]) and torch.equal(other[:, :1], keep[:, :1])
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_norm_every_rest_of_a_row(rh, dtype):
+    """Rows that end anywhere in a piece, at the wave's and the workgroup's ends too; what lies beside a row (NaN) is neither read into it nor
+    written; the residual stream in place."""
+    g = torch.Generator(device="cuda").manual_seed(3)
+    for base in (0, 504, 512, 1016, 2040, 4088, 8184, 16376):
+        for cols in range(base + 1, base + 18):
+            wide = torch.full((5, cols + 13), float("nan"), device="cuda").to(dtype)
+            x = wide[:, 5:5 + cols]
+            x.copy_(torch.randn((5, cols), generator=g, device="cuda"))
+            w = torch.randn(cols, generator=g, device="cuda")
+            r_wide = wide.clone()
+            r = r_wide[:, 5:5 + cols]
+            _check_norm(rh, x, w, r.clone(), 1e-6, "both")
+            want = rh.norm_residual(x, w, r.clone(), outputs="both")
+            got = rh.norm_residual(x, w, r, outputs="both", sum_out=r)
+            assert all(torch.equal(a.view(torch.uint8) if a.dtype == E4M3 else a, b.view(torch.uint8) if b.dtype == E4M3 else b) for a, b in zip(got, want))
+            assert bool(r_wide[:, :5].isnan().all()) and bool(r_wide[:, 5 + cols:].isnan().all())
+
+
 def test_norm_extreme_rows(rh):
     x = torch.zeros((6, 300), device="cuda")
     x[1], x[2, 5], x[3, 7], x[4], x[5] = 1e-30, float("inf"), float("nan"), 1e30, 1e-3
