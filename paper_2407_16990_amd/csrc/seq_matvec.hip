@@ -22,6 +22,7 @@ struct matvec_args {
     int64_t x_stride;
     int32_t rows, outs, ins, blocks;
     int32_t tiles, ks, tw;       // tiles of outputs; waves a tile; tiles a workgroup at a time
+    int32_t threads;             // of a workgroup
     int32_t quads, slice, chunk; // stretches of 512 of the inner index: all, a workgroup's, and as many as x lies in LDS for at a time
     const float* x_scale;
     void* y;
@@ -87,7 +88,8 @@ __device__ __forceinline__ bf16x8 matvec_wide_slow(uint32_t c, uint32_t scale)
     return r.all;
 }
 
-template <int XT, int MT, int R, bool SPLIT>
+// SPLIT: the inner index is cut into slices; ENDS: it is no multiple of 512 (what the others need not look at costs them up to 0.8 us of 14)
+template <int XT, int MT, int R, bool SPLIT, bool ENDS>
 __global__ __launch_bounds__(64 * MATVEC_WAVES(XT, MT)) void k_seq_matvec(matvec_args a)
 {
     typedef matvec_kind<XT> K;
@@ -134,42 +136,73 @@ __global__ __launch_bounds__(64 * MATVEC_WAVES(XT, MT)) void k_seq_matvec(matvec
                 v[d] = u[0]; v[d + 1] = u[1]; v[d + 2] = u[2]; v[d + 3] = u[3];
             }
     };
+    // a row's end that has been loaded as a whole piece, from `by` elements ahead and so still in the row, moved to its place, with zeros behind
+    auto settle = [&](uint32_t (&v)[W], int by) {
+        const int b = by * (int)sizeof(T);                   // bytes
+#pragma unroll
+        for (int d = W / 2; d; d /= 2)
+#pragma unroll
+            for (int k = 0; k < W; ++k) v[k] = b & 4 * d ? k + d < W ? v[k + d] : 0 : v[k];
+        if constexpr (sizeof(T) < 4)
+#pragma unroll
+            for (int k = 0; k < W; ++k) v[k] = __builtin_amdgcn_alignbyte(k + 1 < W ? v[k + 1] : 0, v[k], b & 3);
+    };
+    // piece p of row m, which may hold the row's end, or lie behind it
+    auto get_end = [&](int q0, int m, int p, uint32_t (&v)[W]) {
+        const T* from = (const T*)a.x + (m0 + m) * a.x_stride;
+        const int e = q0 * 512 + p * PIECE, n = a.ins - e;
+        if (n >= PIECE) get(from + e, v);
+        else if (n > 0) {
+            if (XT != RH_T_F32 && a.ins >= PIECE) { get(from + a.ins - PIECE, v); settle(v, PIECE - n); }
+            else
+#pragma unroll
+                for (int d = 0; d < PIECE; ++d) {            // eight words at most, or a row shorter than a piece
+                    const uint32_t bits = d >= n ? 0 : sizeof(T) == 4 ? *(const uint32_t*)(from + e + d) : sizeof(T) == 2 ? *(const uint16_t*)(from + e + d) : *(const uint8_t*)(from + e + d);
+                    v[d * sizeof(T) / 4] |= bits << (8 * sizeof(T) * (d % (4 / sizeof(T))));
+                }
+        }
+    };
     auto stage = [&](int q0, int nq) {
-        const int per_row = nq * 4 * PER_STEP, all = per_row * M;                          // pieces: of a row, of all
-        // i / per_row by a product: (i + 1/2) / per_row is at least 1 / (2 per_row) away from a whole number, and the product's error, below
+        const int per_row = nq * 4 * PER_STEP;               // pieces of a row in LDS
+        int whole = per_row;                                 // and those that the first loop takes
+        if constexpr (ENDS) {
+            const int left = (a.ins - q0 * 512) / PIECE;
+            whole = left >= per_row ? per_row : XT == RH_T_F32 ? 0 : left;
+        }
+        const int all = whole * M;
+        // i / whole by a product: (i + 1/2) / whole is at least 1 / (2 whole) away from a whole number, and the product's error, below
         // 2^-21 of it, stays below that, since i < 2^14 (what fits the LDS)
-        const float inverse = __builtin_amdgcn_rcpf((float)per_row);
-        auto row = [&](int i) { return (int)(((float)i + 0.5f) * inverse); };
-        if ((q0 + nq) * 512 <= a.ins) {
-            constexpr int AHEAD = 4;                         // pieces of a thread in flight
-            for (int first = t; first < all; first += AHEAD * blockDim.x) {
-                uint32_t v[AHEAD][W];
-                int m[AHEAD], p[AHEAD];
+        const float inverse = __builtin_amdgcn_rcpf((float)whole);
+        constexpr int AHEAD = 4;                             // pieces of a thread in flight
+        for (int first = t; first < all; first += AHEAD * a.threads) {
+            uint32_t v[AHEAD][W];
+            int m[AHEAD], p[AHEAD];
 #pragma unroll
-                for (int k = 0; k < AHEAD; ++k) {            // behind the last: the last again
-                    int i = first + k * (int)blockDim.x;
-                    i = i < all ? i : all - 1;
-                    m[k] = row(i); p[k] = i - m[k] * per_row;
-                    get((const T*)a.x + (m0 + m[k]) * a.x_stride + q0 * 512 + p[k] * PIECE, v[k]);
-                }
-#pragma unroll
-                for (int k = 0; k < AHEAD; ++k) put(m[k], p[k], v[k]);
+            for (int k = 0; k < AHEAD; ++k) {                // behind the last: the last again
+                int i = first + k * a.threads;
+                i = i < all ? i : all - 1;
+                m[k] = (int)(((float)i + 0.5f) * inverse); p[k] = i - m[k] * whole;
+                get((const T*)a.x + (m0 + m[k]) * a.x_stride + q0 * 512 + p[k] * PIECE, v[k]);
             }
-        } else
-            for (int i = t; i < all; i += blockDim.x) {      // rows that end in here: zeros behind
-                const int m = row(i), p = i - m * per_row, e = q0 * 512 + p * PIECE, n = a.ins - e;
-                const T* from = (const T*)a.x + (m0 + m) * a.x_stride + e;
-                uint32_t v[W] = {};
-                if (n >= PIECE) get(from, v);
-                else if (n > 0) {
 #pragma unroll
-                    for (int d = 0; d < PIECE; ++d) {
-                        const uint32_t bits = d >= n ? 0 : sizeof(T) == 4 ? *(const uint32_t*)(from + d) : sizeof(T) == 2 ? *(const uint16_t*)(from + d) : *(const uint8_t*)(from + d);
-                        v[d * sizeof(T) / 4] |= bits << (8 * sizeof(T) * (d % (4 / sizeof(T))));
-                    }
-                }
+            for (int k = 0; k < AHEAD; ++k) {
+                // fp32 rows, whose pieces take time to cut: only once (1 x 1024 x 512: 5.2 -> 4.7 us; bf16 rows are slower so, 64 x 1024 x 512 5.6 -> 6.3)
+                if (XT == RH_T_F32 && first + k * a.threads >= all) break;
+                put(m[k], p[k], v[k]);
+            }
+        }
+        if constexpr (ENDS) {
+            // Rows that end in here: the piece with a row's end, and zeros behind it, beginning with the last threads; of fp32 rows all pieces, one at a
+            // time (1 x 1024 x 510: 4.6 us, as the others 5.2; those so: 16 x 4096 x 4090, bf16, 10.0, as they are 7.7).
+            const int rest = per_row - whole;
+            const float inv = __builtin_amdgcn_rcpf((float)rest);
+            for (int i = XT == RH_T_F32 ? t : a.threads - 1 - t; i < rest * M; i += a.threads) {
+                const int m = (int)(((float)i + 0.5f) * inv), p = whole + i - m * rest;
+                uint32_t v[W] = {};
+                get_end(q0, m, p, v);
                 put(m, p, v);
             }
+        }
     };
 
     // ---- a wave's weights: tile by tile of outputs, of each its share of the stretches of every chunk
@@ -201,7 +234,7 @@ __global__ __launch_bounds__(64 * MATVEC_WAVES(XT, MT)) void k_seq_matvec(matvec
             const int b0 = quad * 16;                        // the stretch's first block
             const uint8_t* code = a.w + ((int64_t)n * a.blocks + b0) * 16;
             const uint8_t* scale = a.w_scale + (int64_t)n * a.blocks + b0;
-            if (b0 + 16 <= a.blocks) {
+            if (!ENDS || b0 + 16 <= a.blocks) {
 #pragma unroll
                 for (int s = 0; s < 4; ++s) w.code[r][s] = *(const u32x4*)(code + (4 * s + j) * 16);
                 w.scale[r] = seq_load<u32x4>(scale);
@@ -211,10 +244,9 @@ __global__ __launch_bounds__(64 * MATVEC_WAVES(XT, MT)) void k_seq_matvec(matvec
                     const bool in = b0 + 4 * s + j < a.blocks;   // a block that is none: codes of zero, a scale of one
                     const u32x4 v = *(const u32x4*)(in ? code + (4 * s + j) * 16 : a.w);
                     w.code[r][s] = in ? v : u32x4{0, 0, 0, 0};
-                    uint32_t e = 0;
-#pragma unroll
-                    for (int b = 0; b < 4; ++b) e |= (uint32_t)(b0 + 4 * s + b < a.blocks ? scale[4 * s + b] : 127) << (8 * b);
-                    w.scale[r][s] = e;
+                    // of the scales, the lane's own (one by one with the others of the word: 16 x 1024 x 1000, e4m3 rows, 8.5 us)
+                    const uint32_t e = scale[in ? 4 * s + j : 0];
+                    w.scale[r][s] = (in ? e : 127) << (8 * j);
                 }
             }
         }
@@ -398,7 +430,7 @@ __global__ __launch_bounds__(64 * MATVEC_WAVES(XT, MT)) void k_seq_matvec(matvec
     const int rounds = (a.tiles - (int)blockIdx.x * a.tw + tile_step - 1) / tile_step, vectors = rounds * a.tw * R * MT;
     auto join = [&](auto ahead) __attribute__((always_inline)) {
         constexpr int Z = decltype(ahead)::value, N = 16 / Z;                  // a wave loads Z slices of N vectors at a time
-        for (int n0 = wave * N; n0 < vectors; n0 += (blockDim.x >> 6) * N) {
+        for (int n0 = wave * N; n0 < vectors; n0 += (a.threads >> 6) * N) {
             f32x4 sum[N] = {};
             for (int z = 0; z < a.slices; z += Z) {
                 two v[N][Z];
@@ -436,7 +468,8 @@ static hipError_t launch_matvec(rh_ctx* ctx, matvec_args a)
     typedef matvec_kind<XT> K;
     static bool attr_done[RH_MAX_DEVICES] = {};              // the attribute is per device
     if (!attr_done[ctx->device]) {
-        for (const void* f : {(const void*)k_seq_matvec<XT, MT, R, false>, (const void*)k_seq_matvec<XT, MT, R, true>}) {
+        for (const void* f : {(const void*)k_seq_matvec<XT, MT, R, false, false>, (const void*)k_seq_matvec<XT, MT, R, true, false>,
+                              (const void*)k_seq_matvec<XT, MT, R, false, true>, (const void*)k_seq_matvec<XT, MT, R, true, true>}) {
             const hipError_t e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, MATVEC_LDS);
             if (e != hipSuccess) return e;
         }
@@ -492,10 +525,16 @@ static hipError_t launch_matvec(rh_ctx* ctx, matvec_args a)
     const int64_t pieces = (int64_t)a.chunk * (512 / K::PIECE) * M;
     int waves = a.tw * a.ks;
     while (waves < WAVES && (int64_t)waves * 64 * 8 <= pieces) ++waves;
-    const dim3 grid(groups, gy, a.slices), block(64 * waves);
+    a.threads = 64 * waves;
+    const dim3 grid(groups, gy, a.slices), block(a.threads);
     const size_t lds = whole ? (size_t)a.slice * quad + (a.ks > 1 ? SUMS : 0) : MATVEC_LDS;
-    if (a.slices > 1) hipLaunchKernelGGL((k_seq_matvec<XT, MT, R, true>), grid, block, lds, ctx->stream, a);
-    else hipLaunchKernelGGL((k_seq_matvec<XT, MT, R, false>), grid, block, lds, ctx->stream, a);
+    auto launch = [&](auto split, auto ends) {
+        hipLaunchKernelGGL((k_seq_matvec<XT, MT, R, decltype(split)::value != 0, decltype(ends)::value != 0>), grid, block, lds, ctx->stream, a);
+    };
+    const bool ends = a.ins % 512 != 0;
+    if (a.slices > 1) { if (ends) launch(seq_const<1>(), seq_const<1>()); else launch(seq_const<1>(), seq_const<0>()); }
+    else if (ends) launch(seq_const<0>(), seq_const<1>());
+    else launch(seq_const<0>(), seq_const<0>());
     return hipGetLastError();
 }
 

@@ -544,6 +544,19 @@ def test_matvec_long_rows(rh, dtype, rows, n_out, n_in):
             assert torch.equal(rh.matvec_packed(x, w, sc, x_scale=xs, relu=relu, out_dtype=out), y)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+def test_matvec_every_rest_of_a_row(rh, dtype):
+    """Rows that end anywhere in a piece, block or stretch of 512; what lies beside a row (NaN) does not matter."""
+    g = torch.Generator(device="cuda").manual_seed(9)
+    for base in (0, 500, 1010, 4080):
+        for n_in in range(base + 1, base + 37):
+            w, sc = _weights(g, 20, n_in)
+            x = torch.full((19, n_in + 9), float("nan"), device="cuda").to(dtype)[:, 4:4 + n_in]
+            x.copy_(_rows(g, 19, n_in, dtype))
+            for out in (torch.float32, torch.bfloat16):
+                _check_matvec(rh, x, w, sc, None, False, out)
+
+
 def test_matvec_long_rows_hold_what_is_not_finite(rh):
     """An infinity or NaN of a row stays in that row's outputs, wherever along the row it lies."""
     g = torch.Generator(device="cuda").manual_seed(8)
