@@ -2,7 +2,7 @@
 //
 // Bound by memory: every key and value of a stream is read once for all query heads that share it.  The scores and the sums go on the
 // matrix cores, which have rate to spare even where a tile of 16 heads is mostly empty (64 streams of up to 8192 tokens, bf16, 32 heads
-// on 8 of 128: 207 us, 5.1 TB/s where a copy has 5.2; they work 5 % of the time), so that one kernel serves every number of heads a key,
+// on 8 of 128: 204 us, 5.2 TB/s, as much as a copy has; they work 5 % of the time), so that one kernel serves every number of heads a key,
 // and vector instructions are left for the softmax.
 //
 // A wave takes a tile of tokens (32; 16 of an fp32 cache) at a time, with no barrier in its loop:

@@ -3,8 +3,8 @@
 // Bound by memory: x and the residual are read once, the sum, y and its 8-bit form written once.  A row stays in the
 // registers of the waves that own it: the mean square, and then the largest |y|, are sums and maxima over them.
 // A row belongs to one wave where it is short, so that a workgroup of four waves needs no barrier.
-// 14720 x 4095 of fp32, all outputs: 186 us, 5.5 TB/s; of bf16 127, 4.3 TB/s (rows at odd addresses; 4092: 108, 5.0 TB/s); 8 x 1024 of
-// bf16 4.3, hardly more than an empty launch and two ways to memory.
+// 14720 x 4095 of fp32, all outputs: 183 us, 5.6 TB/s; of bf16 126, 4.3 TB/s (rows at odd addresses; 4092: 108, 5.0 TB/s); 8 x 1024 of
+// bf16, 8-bit output, 3.5, hardly more than an empty launch and a way to memory.
 #include "seq_common.h"
 
 struct norm_args {
