@@ -290,7 +290,8 @@ __global__ __launch_bounds__(ATTEND_T, D <= 128 ? 2 : 1) void k_seq_attend(atten
         load_k(now);
         load_v(now);
         int32_t next_entry = entry(tile + turn);
-        for (; tile < tile_end; tile += turn) {
+        auto step = [&](auto has_next) __attribute__((always_inline)) {
+            constexpr bool MORE = decltype(has_next)::value != 0;
             // scores: rows 4*j + i of token tile tt, head c
             stage_k();
             f32x4 sc[TT];
@@ -323,10 +324,14 @@ __global__ __launch_bounds__(ATTEND_T, D <= 128 ? 2 : 1) void k_seq_attend(atten
                     product(wide(u.x, u.y), RB / 64 * 2);
                 }
             }
-            // the next tile's keys, into the registers that the products have read (behind the last tile: page 0's first line, unused)
-            const where next = place(tile + turn, next_entry);
-            load_k(next);
-            const int32_t after = entry(tile + 2 * turn);
+            // the next tile's keys, into the registers that the products have read
+            where next;
+            int32_t after;
+            if constexpr (MORE) {
+                next = place(tile + turn, next_entry);
+                load_k(next);
+                after = entry(tile + 2 * turn);
+            }
 
             // softmax over this tile: token 16*tt + 4*j + i is lane (16*tt + 4*j + i)'s
             float p[ROWS], vs[ROWS], most = -INFINITY;
@@ -402,10 +407,14 @@ __global__ __launch_bounds__(ATTEND_T, D <= 128 ? 2 : 1) void k_seq_attend(atten
                     acc[i + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vb, pl, acc[i + 1], 0, 0, 0);
                 }
             }
-            load_v(next);
-            now = next;
-            next_entry = after;
-        }
+            if constexpr (MORE) {
+                load_v(next);
+                now = next;
+                next_entry = after;
+            }
+        };
+        for (; tile + turn < tile_end; tile += turn) step(seq_const<1>());
+        step(seq_const<0>());
     }
 
     // ---- joining: one set of sums, maximum and total (of this lane's tokens) with another of the same lane
@@ -418,9 +427,11 @@ __global__ __launch_bounds__(ATTEND_T, D <= 128 ? 2 : 1) void k_seq_attend(atten
 #pragma unroll
         for (int i = 0; i < NT; ++i) acc[i] = acc[i] * f + other(i) * g;
     };
+    const int busy = solo ? 1 : tile_end - split * chunk;    // tiles of the chunk, and so waves that had any
     auto join_waves = [&]() __attribute__((always_inline)) {               // into wave 0
 #pragma unroll
         for (int n = ATTEND_WAVES / 2; n; n >>= 1) {
+            if (n >= busy) continue;
             // wave 1 hands over where only it has read
             if (wave >= n && wave < 2 * n) {
                 f32x4(*o)[64] = s_acc[n == 1 ? 1 : wave - n];
@@ -467,7 +478,7 @@ __global__ __launch_bounds__(ATTEND_T, D <= 128 ? 2 : 1) void k_seq_attend(atten
         }
     };
 
-    if (!solo) {
+    if (busy > 1) {
         __syncthreads();                                     // no wave needs its keys any more
         join_waves();
     }
