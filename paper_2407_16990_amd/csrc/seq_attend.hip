@@ -40,6 +40,7 @@ struct attend_args {
 #define ATTEND_WAVES 4
 #define ATTEND_T (64 * ATTEND_WAVES)
 #define ATTEND_CHUNK_MIN 4       // tiles
+#define ATTEND_WHOLE 8           // tiles, where no stream has more
 #define ATTEND_CHUNK_FEW 32      // tiles a chunk up to which each CU gets one chunk; beyond, ATTEND_CHUNKS
 #define ATTEND_SOLO 8            // tiles of a stream that a wave takes alone, where there are many such streams and none longer
 #define ATTEND_GROUPED 64        // chunks of all streams from which on a chunk's units go to one XCD
@@ -119,20 +120,23 @@ __global__ __launch_bounds__(ATTEND_T, D <= 128 ? 2 : 1) void k_seq_attend(atten
     // Many short streams: a wave each, with nothing to join.  (128 streams of up to 256 tokens, 8 heads: 24.0 -> 19.5 us, of up to 64
     // 16.7 -> 10.0.  Half as many streams gain up to fewer tiles: 64 of up to 30 tokens 7.1 -> 6.0, of up to 128 10.7 -> 12.2.)
     const int few = a.n_streams * units / a.n_cu, cap = few < 4 ? few / 2 : ATTEND_SOLO;
-    bool longer = __any(most_tiles > cap);
+    bool longer = __any(most_tiles > cap), several = __any(most_tiles > ATTEND_WHOLE);
     some = seq_sum(some);
     if constexpr (MANY) {
-        if (lane == 0) { s_some[wave] = some; s_most[wave] = longer; }
+        if (lane == 0) { s_some[wave] = some; s_most[wave] = longer + 2 * several; }
         __syncthreads();
-        some = 0.f; longer = false;
+        some = 0.f; longer = several = false;
 #pragma unroll
-        for (int w = 0; w < ATTEND_WAVES; ++w) { some += s_some[w]; longer |= s_most[w] != 0; }
+        for (int w = 0; w < ATTEND_WAVES; ++w) { some += s_some[w]; longer |= s_most[w] & 1; several |= s_most[w] >> 1; }
     }
     const bool solo = !longer;
     const float all = some * (float)units, cus = (float)a.n_cu;
     // at most 2^30, which no stream has (a length is below 2^31, a tile 16 or more): the sums' rounding and their size are both covered
     int chunk = (int)fminf(ceilf(fmaxf(fminf(all / cus, (float)ATTEND_CHUNK_FEW), all / (cus * ATTEND_CHUNKS) * 1.0001f)), 0x1p30f);
-    chunk = solo ? ATTEND_SOLO : ((chunk < ATTEND_CHUNK_MIN ? ATTEND_CHUNK_MIN : chunk) + ATTEND_WAVES - 1) / ATTEND_WAVES * ATTEND_WAVES;
+    // Two tiles a wave take less than a join where no stream has more (8 streams of up to 200 tokens, bf16, 2 heads of 128 8.9 -> 8.2 us; with
+    // streams of 300 among them 9.1 -> 10.5; fp32, 8 heads of 64, 100 tokens 7.7 -> 6.9, of 192, 93 tokens 11.5 -> 12.1: tiles of long rows take longer)
+    const int least = !several && RB <= 512 ? ATTEND_WHOLE : ATTEND_CHUNK_MIN;
+    chunk = solo ? ATTEND_SOLO : ((chunk < least ? least : chunk) + ATTEND_WAVES - 1) / ATTEND_WAVES * ATTEND_WAVES;
     // a stream without tokens has one chunk, which writes its zeros; only chunks of streams that have several need scratch memory
     int32_t n_chunks[PER], mine = 0, shared = 0;
 #pragma unroll
