@@ -2,7 +2,7 @@
 //
 // Bound by memory: x and the residual are read once, the sum, y and its 8-bit form written once.  A row stays in the
 // registers of the waves that own it: the mean square, and then the largest |y|, are sums and maxima over them.
-// A row belongs to one wave where it is short, so that a workgroup of four waves needs no barrier.
+// A row belongs to one wave where it is short, so that a workgroup of four waves needs no barrier, or to a part of one where it is shorter still.
 // 14720 x 4095 of fp32, all outputs: 183 us, 5.6 TB/s; of bf16 126, 4.3 TB/s (rows at odd addresses; 4092: 108, 5.0 TB/s); 8 x 1024 of
 // bf16, 8-bit output, 3.5, hardly more than an empty launch and a way to memory.
 #include "seq_common.h"
@@ -73,13 +73,13 @@ __device__ __forceinline__ void norm_store(T* p, int n, const float (&v)[E])
     norm_put<(int)sizeof(T)>((uint8_t*)p, n * (int)sizeof(T), w);
 }
 
-// The sum (MAX: the largest, a NaN staying) of a value of every thread of a row's WAVES waves.
-template <int WAVES, bool MAX>
+// The sum (MAX: the largest, a NaN staying) of a value of every thread of a row's WAVES waves, or of its LANES lanes.
+template <int WAVES, int LANES, bool MAX>
 __device__ __forceinline__ float norm_over(float v, float* s_part)
 {
     auto both = [](float a, float b) { return MAX ? (b != b || b > a ? b : a) : a + b; };
 #pragma unroll
-    for (int o = 32; o; o >>= 1) v = both(v, __shfl_xor(v, o));
+    for (int o = LANES / 2; o; o >>= 1) v = both(v, __shfl_xor(v, o));
     if constexpr (WAVES > 1) {
         if ((threadIdx.x & 63) == 0) s_part[threadIdx.x >> 6] = v;
         __syncthreads();
@@ -91,14 +91,15 @@ __device__ __forceinline__ float norm_over(float v, float* s_part)
     return v;
 }
 
-template <typename T, int WAVES, int ITEMS>
+// a row's WAVES waves, of one of them LANES lanes, with ITEMS pieces a thread
+template <typename T, int WAVES, int LANES, int ITEMS>
 __global__ __launch_bounds__(WAVES > 1 ? WAVES * 64 : 256) void k_seq_norm(norm_args a)
 {
-    constexpr int E = 16 / sizeof(T), NT = WAVES * 64, PER = WAVES > 1 ? 1 : 4;       // threads a row, rows a workgroup
+    constexpr int E = 16 / sizeof(T), NT = WAVES * LANES, PER = WAVES > 1 ? 1 : 256 / LANES;       // threads a row, rows a workgroup
     __shared__ float s_part[WAVES > 1 ? WAVES * PER : 1];
     const int t = threadIdx.x % NT, sub = threadIdx.x / NT;
     const int row = blockIdx.x * PER + sub;
-    if (PER > 1 && row >= a.rows) return;                    // PER > 1 only where a row is one wave's: no barrier is left behind
+    if (PER > 1 && row >= a.rows) return;                    // PER > 1 only where a row is one wave's or less: no barrier is left behind
     const T* x = (const T*)a.x + row * a.x_stride;
     const T* r = (const T*)a.residual + row * a.residual_stride;
     float v[ITEMS][E], square = 0.f;
@@ -124,7 +125,7 @@ __global__ __launch_bounds__(WAVES > 1 ? WAVES * 64 : 256) void k_seq_norm(norm_
     for (int i = 0; i < ITEMS; ++i)
 #pragma unroll
         for (int e = 0; e < E; ++e) square += v[i][e] * v[i][e];
-    square = norm_over<WAVES, false>(square, s_part);
+    square = norm_over<WAVES, LANES, false>(square, s_part);
     if (a.sum) {
         T* s = (T*)a.sum + row * a.sum_stride;
 #pragma unroll
@@ -165,7 +166,7 @@ __global__ __launch_bounds__(WAVES > 1 ? WAVES * 64 : 256) void k_seq_norm(norm_
         }
     }
     if (!a.y8) return;
-    most = norm_over<WAVES, true>(most, s_part);
+    most = norm_over<WAVES, LANES, true>(most, s_part);
     most = most < SEQ_AMAX_MIN ? SEQ_AMAX_MIN : most;
     const float inv = SEQ_E4M3_MAX / most;
     if (t == 0) a.y8_scale[row] = most / SEQ_E4M3_MAX;
@@ -188,18 +189,22 @@ static void launch_norm(hipStream_t s, const norm_args& a)
 {
     constexpr int E = 16 / sizeof(T);
     const int pieces = (a.cols + E - 1) / E;                 // of 16 bytes, one a thread and item
-#define N(WAVES, ITEMS) hipLaunchKernelGGL((k_seq_norm<T, WAVES, ITEMS>), dim3(WAVES > 1 ? a.rows : (a.rows + 3) / 4), \
-                                           dim3(WAVES > 1 ? WAVES * 64 : 256), 0, s, a)
+#define N(WAVES, LANES, ITEMS) hipLaunchKernelGGL((k_seq_norm<T, WAVES, LANES, ITEMS>), dim3(WAVES > 1 ? a.rows : (a.rows + 256 / LANES - 1) / (256 / LANES)), \
+                                                  dim3(WAVES > 1 ? WAVES * 64 : 256), 0, s, a)
+    // Short rows share a wave (16050 rows of 60, fp32: 10.7 -> 5.9 us, of 200 in bf16 13.3 -> 10.0).
+    if (pieces <= 8) N(1, 8, 1);
+    else if (pieces <= 16) N(1, 16, 1);
+    else if (pieces <= 32) N(1, 32, 1);
+    else if (pieces <= 64) N(1, 64, 1);
     // Two pieces a thread while a workgroup's waves last.  8 rows of 1800 in bf16: 4.7 us, with four a thread in one wave 6.3, with one a thread 4.4; 14720 of 1024 in fp32
     // 43.5, 43.5, 47.5; 1000 of 4095 in fp32 13.5, 13.6, 16.7.  A single row of 8000 in bf16 4.9, 5.8, 5.3.
-    if (pieces <= 64) N(1, 1);
-    else if (pieces <= 128) N(1, 2);
-    else if (pieces <= 256) N(2, 2);
-    else if (pieces <= 512) N(4, 2);
-    else if (pieces <= 1024) N(8, 2);
-    else if (pieces <= 2048) N(8, 4);
-    else if (pieces <= 4096) N(16, 4);
-    else if constexpr (E == 4) N(16, 8);                     // of bf16 none is that long
+    else if (pieces <= 128) N(1, 64, 2);
+    else if (pieces <= 256) N(2, 64, 2);
+    else if (pieces <= 512) N(4, 64, 2);
+    else if (pieces <= 1024) N(8, 64, 2);
+    else if (pieces <= 2048) N(8, 64, 4);
+    else if (pieces <= 4096) N(16, 64, 4);
+    else if constexpr (E == 4) N(16, 64, 8);                     // of bf16 none is that long
 #undef N
 }
 

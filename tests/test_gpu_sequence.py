@@ -469,6 +469,29 @@ def test_norm_every_rest_of_a_row(rh, dtype):
             assert bool(r_wide[:, :5].isnan().all()) and bool(r_wide[:, 5 + cols:].isnan().all())
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_norm_short_rows_side_by_side(rh, dtype):
+    """Rows that share a wave keep to themselves: a NaN, an infinity or zeros in one change no other."""
+    g = torch.Generator(device="cuda").manual_seed(11)
+    for rows in (1, 3, 37, 300):
+        for cols in (1, 7, 30, 32, 33, 63, 64, 65, 100, 128, 129, 200, 256, 257):
+            x = torch.randn((rows, cols), generator=g, device="cuda").to(dtype)
+            w = torch.rand(cols, generator=g, device="cuda") + 0.5
+            _check_norm(rh, x, w, None, 1e-6, "both")
+            want = rh.norm_residual(x, w, outputs="both")
+            bad = x.clone()
+            bad[1::4, cols // 2] = float("nan")
+            bad[2::8, -1] = float("inf")
+            bad[3::8] = 0
+            got = rh.norm_residual(bad, w, outputs="both")
+            same = torch.ones(rows, dtype=torch.bool, device="cuda")
+            same[1::4] = False; same[2::8] = False; same[3::8] = False
+            for a, b in zip(got[1:], want[1:]):                     # without a residual there is no sum
+                a, b = a[same], b[same]
+                assert torch.equal(a.view(torch.uint8) if a.dtype == E4M3 else a, b.view(torch.uint8) if b.dtype == E4M3 else b)
+            assert bool(got[1][1::4].isnan().all()) and bool((got[1][3::8] == 0).all())
+
+
 def test_norm_extreme_rows(rh):
     x = torch.zeros((6, 300), device="cuda")
     x[1], x[2, 5], x[3, 7], x[4], x[5] = 1e-30, float("inf"), float("nan"), 1e30, 1e-3
