@@ -521,10 +521,12 @@ static hipError_t launch_matvec(rh_ctx* ctx, matvec_args a)
         }
     }
     cut(best);
-    // waves, and as many more as have eight pieces of x each to lay out
+    // waves, and as many more as have pieces of x to lay out, four a thread; two of fp32 rows, which are cut (16 x 1024 x 510: eight 7.7 us, four 6.5,
+    // two 5.7; bf16 rows, 16 x 1024 x 512, 4.4, 4.3, 4.6, 64 x 1024 x 510 6.1, 5.5, 5.5)
+    constexpr int SHARE = 64 * (XT == RH_T_F32 ? 2 : 4);
     const int64_t pieces = (int64_t)a.chunk * (512 / K::PIECE) * M;
     int waves = a.tw * a.ks;
-    while (waves < WAVES && (int64_t)waves * 64 * 8 <= pieces) ++waves;
+    while (waves < WAVES && (int64_t)waves * SHARE <= pieces) ++waves;
     a.threads = 64 * waves;
     const dim3 grid(groups, gy, a.slices), block(a.threads);
     const size_t lds = whole ? (size_t)a.slice * quad + (a.ks > 1 ? SUMS : 0) : MATVEC_LDS;
