@@ -216,10 +216,10 @@ extern "C" rh_status rh_cache_plan(rh_ctx* ctx, const int32_t* n_new, const int3
 // ---------------------------------------------------------------------------------------------------------------
 // rh_cache_write
 // ---------------------------------------------------------------------------------------------------------------
-// Bound by memory: every key and value read and written once (27600 tokens of 8 heads of 128, bf16 to e4m3: 171 MB in 38 to 44 us, 3.9 to 4.5 TB/s; half the
+// Bound by memory: every key and value read and written once (27600 tokens of 8 heads of 128, bf16 to e4m3: 171 MB in 40 to 46 us, 3.7 to 4.3 TB/s; half the
 // bytes written go to scattered slots, a quarter of a KB at a time).  G lanes (a power of two) take a head's row, eight elements each, so
 // that the largest magnitude is a few lane exchanges; lanes past the head's size idle.
-// Rows a thread, whose loads are in flight together: two where they are quantised (27600 tokens of 8 heads of 128: 44.1 us, one row
+// Rows a thread, whose loads are in flight together: two where they are quantised (27600 tokens of 8 heads of 128, with quotients not yet corrected: 44.1 us, one row
 // 48.7, four 47.1), else one (bf16 46.0, two 48.2; 64 tokens 2.2 and 2.4).
 template <typename C> constexpr int write_rows() { return sizeof(C) == 1 ? 2 : 1; }
 
@@ -284,11 +284,9 @@ __global__ __launch_bounds__(256) void k_seq_write(write_args a)
 #pragma unroll
             for (int o = G / 2; o; o >>= 1) { const float u = __shfl_xor(most, o); most = u != u || u > most ? u : most; }
             most = most < SEQ_AMAX_MIN ? SEQ_AMAX_MIN : most;
-            const float inv = SEQ_E4M3_MAX / most;
-            if (g == 0) a.scale[kv][((int64_t)p * a.heads.d + head[i]) * a.page.d + line] = most / SEQ_E4M3_MAX;
-            uint2 q;
-            q.x = seq_pack_e4m3(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
-            q.y = seq_pack_e4m3(v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv);
+            const seq_scale scale = seq_make_scale(most);
+            if (g == 0) a.scale[kv][((int64_t)p * a.heads.d + head[i]) * a.page.d + line] = scale.value;
+            const uint2 q = make_uint2(seq_pack_scaled(v[0], v[1], v[2], v[3], scale), seq_pack_scaled(v[4], v[5], v[6], v[7], scale));
             // past the L2, where the scales' lines, of which each store fills a word, then stay until they are full (44.3 -> 42.8 us)
             if (in) __builtin_nontemporal_store((uint64_t)q.y << 32 | q.x, (uint64_t*)((uint8_t*)a.dst[kv] + at));
         } else if constexpr (sizeof(C) == 2) {

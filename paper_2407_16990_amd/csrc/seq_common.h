@@ -34,6 +34,18 @@ __device__ __forceinline__ uint32_t seq_pack_e4m3(float a, float b, float c, flo
     return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, r, true);
 }
 
+// Four values over their scale, as e4m3.  Each quotient is rounded once, as a division's: the product with the reciprocal, corrected by its remainder (a fused
+// multiplication leaves it exact), is that quotient wherever neither underflows; other scales are divided by.  (27600 tokens of 8 heads
+// of 128 written in 46.1 us; divisions for all 52.7; products alone 43.7, which put what lies at a tie between two codes on either side.)
+struct seq_scale { float value, inverse; };
+__device__ __forceinline__ seq_scale seq_make_scale(float most) { const float v = most / SEQ_E4M3_MAX; return {v, 1.f / v}; }
+__device__ __forceinline__ uint32_t seq_pack_scaled(float a, float b, float c, float d, const seq_scale& s)
+{
+    if (!(s.value >= 0x1p-90f && s.value <= 0x1p120f)) return seq_pack_e4m3(a / s.value, b / s.value, c / s.value, d / s.value);
+    auto over = [&](float v) { const float q = v * s.inverse; return fmaf(fmaf(-q, s.value, v), s.inverse, q); };
+    return seq_pack_e4m3(over(a), over(b), over(c), over(d));
+}
+
 template <int N> struct seq_const { static constexpr int value = N; };
 
 // Inclusive running sum over the wave's lanes, by row shifts and row broadcasts of the vector ALU.

@@ -4,7 +4,7 @@
 // registers of the waves that own it: the mean square, and then the largest |y|, are sums and maxima over them.
 // A row belongs to one wave where it is short, so that a workgroup of four waves needs no barrier, or to a part of one where it is shorter still.
 // 14720 x 4095 of fp32, all outputs: 183 us, 5.6 TB/s; of bf16 126, 4.3 TB/s (rows at odd addresses; 4092: 108, 5.0 TB/s); 8 x 1024 of
-// bf16, 8-bit output, 3.5, hardly more than an empty launch and a way to memory.
+// bf16, 8-bit output, 3.7, hardly more than an empty launch and a way to memory.
 #include "seq_common.h"
 
 struct norm_args {
@@ -168,8 +168,8 @@ __global__ __launch_bounds__(WAVES > 1 ? WAVES * 64 : 256) void k_seq_norm(norm_
     if (!a.y8) return;
     most = norm_over<WAVES, LANES, true>(most, s_part);
     most = most < SEQ_AMAX_MIN ? SEQ_AMAX_MIN : most;
-    const float inv = SEQ_E4M3_MAX / most;
-    if (t == 0) a.y8_scale[row] = most / SEQ_E4M3_MAX;
+    const seq_scale y8_scale = seq_make_scale(most);
+    if (t == 0) a.y8_scale[row] = y8_scale.value;
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
         const int c = (t + i * NT) * E, n = a.cols - c;
@@ -177,7 +177,7 @@ __global__ __launch_bounds__(WAVES > 1 ? WAVES * 64 : 256) void k_seq_norm(norm_
         uint8_t* o = a.y8 + (int64_t)row * a.cols + c;
         u32x4 q = {0, 0, 0, 0};
 #pragma unroll
-        for (int e = 0; e < E; e += 4) q[e / 4] = seq_pack_e4m3(v[i][e] * inv, v[i][e + 1] * inv, v[i][e + 2] * inv, v[i][e + 3] * inv);
+        for (int e = 0; e < E; e += 4) q[e / 4] = seq_pack_scaled(v[i][e], v[i][e + 1], v[i][e + 2], v[i][e + 3], y8_scale);
         if (n < E) norm_put<1>(o, n, q);
         else if constexpr (E == 8) seq_store(o, make_uint2(q[0], q[1]));
         else seq_store(o, q[0]);
