@@ -104,8 +104,7 @@ rh_status rh_norm_residual(rh_ctx* ctx, const void* x, int64_t x_stride, const v
 
 /*
  * y[m][n] = x_scale[m] * sum_k x[m][k] * w[n][k], optionally ReLU, for a few rows m: weights are read once for 16 of them (fp32), for
- * 32 (bf16; e4m3 with an fp32 output or fewer than 512 inputs), for 64 (e4m3 otherwise: products of the scaled 8-bit kind, whose partial
- * sums are off by some 2^-18 of the result's norm, a five-hundredth of the bf16 output's rounding).
+ * 32 (bf16, e4m3).
  *   w (dev) u8 [n_out][16*ceil(n_in/32)], 16-byte aligned: codes of 4 bits, even k in the low half; code c stands for
  *   {0, 1/2, 1, 3/2, 2, 3, 4, 6}[c & 7], negative with bit 3.  w_scale (dev) u8 [n_out][ceil(n_in/32)]: 32 codes
  *   share the factor 2^(scale - 127) (255 is not a number).  Codes past n_in do not matter.

@@ -6,13 +6,12 @@
 //   bf16 rows   8 codes at a time become bf16 values, their block's scale included (a conversion of the hardware; exact)
 //   fp32 rows   the same against x cut into three bf16 parts, which together are x exactly: products of full precision at three
 //               products of the 16-bit rate, where the fp32 rate is a sixteenth of it
-//   e4m3 rows   as bf16 rows, which hold them exactly; or the scaled product of 8-bit and 4-bit values, which takes codes, scales and rows
-//               as they are.  That one keeps fewer bits of its partial sums: against 64 bits, 2000 x 8 outputs of 32 / 512 / 8192 terms
-//               are 1.3e-6 / 3.5e-6 / 4.2e-6 off in norm, 0 / 3e-8 / 7e-8 as bf16 rows.  So it serves bf16 outputs only, whose
-//               rounding is 1.7e-3, and from one whole stretch of 512 terms on, where there is something to gain
+//   e4m3 rows   as bf16 rows, which hold them exactly.  (The scaled product of 8-bit and 4-bit values would take codes, scales and rows as they
+//               are - 10.1 us for the 12.5 below - but keeps fewer than 32 bits of its partial sums: two pairs of +-448 that cancel in a row of 8192 small terms
+//               left 1.2 where the sum is -0.03.)
 // A workgroup's waves share out its tiles of outputs and the inner index (KS waves a tile, summed in LDS in order), so that few outputs
 // still use every wave; where x is long or the tiles are few, workgroups share the inner index too, and the last of them adds up their sums, in their order.
-// 16 x 16384 x 4096, e4m3 rows: 10.1 us, 3.5 TB/s of weights; 7.0 at a copy's rate, about 2 until the first bytes are there, the rest x.  1 x 1024 x 510,
+// 16 x 16384 x 4096, e4m3 rows: 12.5 us, 2.9 TB/s of weights; 7.0 at a copy's rate, about 2 until the first bytes are there, the rest x.  1 x 1024 x 510,
 // fp32: 4.0, hardly more than an empty launch (2.5) and one way to memory.
 #include "seq_common.h"
 
@@ -34,17 +33,14 @@ struct matvec_args {
 };
 
 #define MATVEC_WAVES(XT, MT) (MT == 1 && XT != RH_T_F32 ? 16 : 8)       // of a workgroup, one a CU; the others' registers allow eight
+#define MATVEC_PIECE 8           // elements of x in 16 bytes of LDS
 #define MATVEC_LDS (160 * 1024)
 #define MATVEC_HUGE 252          // scales from here on can take a code past the largest bf16 number
 
-typedef __attribute__((__vector_size__(8 * sizeof(int)))) int i32x8;
-
 template <int XT> struct matvec_kind;
-template <> struct matvec_kind<RH_T_F32> { typedef float T; static constexpr int PARTS = 3, PIECE = 8; };
-template <> struct matvec_kind<RH_T_BF16> { typedef __bf16 T; static constexpr int PARTS = 1, PIECE = 8; };
-template <> struct matvec_kind<RH_T_E4M3> { typedef uint8_t T; static constexpr int PARTS = 1, PIECE = 8; };       // PIECE: elements of x in 16 bytes of LDS
-#define MATVEC_SCALED 3          // e4m3 rows on the scaled product
-template <> struct matvec_kind<MATVEC_SCALED> { typedef uint8_t T; static constexpr int PARTS = 1, PIECE = 16; };
+template <> struct matvec_kind<RH_T_F32> { typedef float T; static constexpr int PARTS = 3; };
+template <> struct matvec_kind<RH_T_BF16> { typedef __bf16 T; static constexpr int PARTS = 1; };
+template <> struct matvec_kind<RH_T_E4M3> { typedef uint8_t T; static constexpr int PARTS = 1; };
 
 // x = the sum of three bf16 numbers, for any finite x: cut off, not rounded, so that none passes the largest
 __device__ __forceinline__ void matvec_cut(float x, uint32_t (&part)[3])
@@ -94,7 +90,7 @@ __global__ __launch_bounds__(64 * MATVEC_WAVES(XT, MT)) void k_seq_matvec(matvec
 {
     typedef matvec_kind<XT> K;
     typedef typename K::T T;
-    constexpr int PARTS = K::PARTS, PIECE = K::PIECE, PER_STEP = 128 / PIECE;      // 16-byte pieces of a row in a step of 128
+    constexpr int PARTS = K::PARTS, PIECE = MATVEC_PIECE, PER_STEP = 128 / PIECE;      // 16-byte pieces of a row in a step of 128
     extern __shared__ uint4 s_mem[];
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6, c = lane & 15, j = lane >> 4;
     const int tw = wave / a.ks, ks = wave % a.ks;
@@ -109,9 +105,9 @@ __global__ __launch_bounds__(64 * MATVEC_WAVES(XT, MT)) void k_seq_matvec(matvec
 
     constexpr int W = PIECE * sizeof(T) / 4;                 // words of a piece in memory
     auto put = [&](int m, int p, const uint32_t* v) {        // piece p of row m
-        // bf16: lane quarter j of the e-th product of a step reads block j's piece e; the scaled product has pieces j and 4 + j there
+        // lane quarter j of the e-th product of a step reads block j's piece e
         const int step = p / PER_STEP, in = p % PER_STEP;
-        u32x4* to = xs + (step * PER_STEP + (XT == MATVEC_SCALED ? in : in % 4 * 4 + in / 4)) * P + m;
+        u32x4* to = xs + (step * PER_STEP + in % 4 * 4 + in / 4) * P + m;
         if constexpr (XT == RH_T_F32) {
             uint32_t w[3][4];
 #pragma unroll
@@ -261,66 +257,48 @@ __global__ __launch_bounds__(64 * MATVEC_WAVES(XT, MT)) void k_seq_matvec(matvec
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
             const u32x4* x = xs + (q * 4 + s) * PER_STEP * P;
-            if constexpr (XT == MATVEC_SCALED) {
-                i32x8 xb[MT];
+            uint32_t scale[R];
+            bool huge = false;
 #pragma unroll
-                for (int i = 0; i < MT; ++i) {
-                    const u32x4 lo = x[mrow[i]], hi = x[4 * P + mrow[i]];
-                    xb[i] = i32x8{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
-                }
+            for (int r = 0; r < R; ++r) { scale[r] = w.scale[r][s] >> (8 * j) & 255; huge |= scale[r] >= MATVEC_HUGE; }
+            if (!__any(huge)) {
 #pragma unroll
-                for (int r = 0; r < R; ++r) {
-                    const u32x4 u = w.code[r][s];
-                    const i32x8 wa = {(int)u[0], (int)u[1], (int)u[2], (int)u[3], 0, 0, 0, 0};
-                    const int scale = (int)(w.scale[r][s] >> (8 * j));
+                for (int e = 0; e < 4; ++e) {
+                    bf16x8 wa[R];
 #pragma unroll
-                    for (int i = 0; i < MT; ++i)
-                        acc[r][i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wa, xb[i], acc[r][i], 4, 0, 0, scale, 0, 127);
+                    for (int r = 0; r < R; ++r) wa[r] = matvec_wide(w.code[r][s][e], scale[r]);
+#pragma unroll
+                    for (int p = PARTS - 1; p >= 0; --p)
+#pragma unroll
+                        for (int i = 0; i < MT; ++i) {
+                            const bf16x8 xb = __builtin_bit_cast(bf16x8, x[p * part_pieces + e * 4 * P + mrow[i]]);
+#pragma unroll
+                            for (int r = 0; r < R; ++r) acc[r][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wa[r], xb, acc[r][i], 0, 0, 0);
+                        }
                 }
             } else {
-                uint32_t scale[R];
-                bool huge = false;
+                // codes that bf16 cannot hold: this step's products by 2^-8, on their own
+                f32x4 part[R][MT];
 #pragma unroll
-                for (int r = 0; r < R; ++r) { scale[r] = w.scale[r][s] >> (8 * j) & 255; huge |= scale[r] >= MATVEC_HUGE; }
-                if (!__any(huge)) {
+                for (int r = 0; r < R; ++r)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        bf16x8 wa[R];
+                    for (int i = 0; i < MT; ++i) part[r][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+                for (int e = 0; e < 4; ++e)
 #pragma unroll
-                        for (int r = 0; r < R; ++r) wa[r] = matvec_wide(w.code[r][s][e], scale[r]);
+                    for (int r = 0; r < R; ++r) {
+                        const uint32_t code = e == 0 ? w.code[r][s][0] : e == 1 ? w.code[r][s][1] : e == 2 ? w.code[r][s][2] : w.code[r][s][3];
+                        const bf16x8 wa = matvec_wide_slow(code, scale[r]);
 #pragma unroll
                         for (int p = PARTS - 1; p >= 0; --p)
 #pragma unroll
-                            for (int i = 0; i < MT; ++i) {
-                                const bf16x8 xb = __builtin_bit_cast(bf16x8, x[p * part_pieces + e * 4 * P + mrow[i]]);
-#pragma unroll
-                                for (int r = 0; r < R; ++r) acc[r][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wa[r], xb, acc[r][i], 0, 0, 0);
-                            }
+                            for (int i = 0; i < MT; ++i)
+                                part[r][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wa, __builtin_bit_cast(bf16x8, x[p * part_pieces + e * 4 * P + mrow[i]]), part[r][i], 0, 0, 0);
                     }
-                } else {
-                    // codes that bf16 cannot hold: this step's products by 2^-8, on their own
-                    f32x4 part[R][MT];
 #pragma unroll
-                    for (int r = 0; r < R; ++r)
+                for (int r = 0; r < R; ++r)
 #pragma unroll
-                        for (int i = 0; i < MT; ++i) part[r][i] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll 1
-                    for (int e = 0; e < 4; ++e)
-#pragma unroll
-                        for (int r = 0; r < R; ++r) {
-                            const uint32_t code = e == 0 ? w.code[r][s][0] : e == 1 ? w.code[r][s][1] : e == 2 ? w.code[r][s][2] : w.code[r][s][3];
-                            const bf16x8 wa = matvec_wide_slow(code, scale[r]);
-#pragma unroll
-                            for (int p = PARTS - 1; p >= 0; --p)
-#pragma unroll
-                                for (int i = 0; i < MT; ++i)
-                                    part[r][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wa, __builtin_bit_cast(bf16x8, x[p * part_pieces + e * 4 * P + mrow[i]]), part[r][i], 0, 0, 0);
-                        }
-#pragma unroll
-                    for (int r = 0; r < R; ++r)
-#pragma unroll
-                        for (int i = 0; i < MT; ++i) acc[r][i] += part[r][i] * 256.f;
-                }
+                    for (int i = 0; i < MT; ++i) acc[r][i] += part[r][i] * 256.f;
             }
         }
     };
@@ -475,7 +453,7 @@ static hipError_t launch_matvec(rh_ctx* ctx, matvec_args a)
         }
         attr_done[ctx->device] = true;
     }
-    const int M = a.rows < 16 * MT ? a.rows : 16 * MT, quad = K::PARTS * 512 / K::PIECE * 16 * (M | 1);       // bytes of x in LDS, of a stretch
+    const int M = a.rows < 16 * MT ? a.rows : 16 * MT, quad = K::PARTS * 512 / MATVEC_PIECE * 16 * (M | 1);       // bytes of x in LDS, of a stretch
     constexpr int WAVES = MATVEC_WAVES(XT, MT), SUMS = WAVES * R * MT * 64 * (int)sizeof(f32x4);
     const int gy = (a.rows + 16 * MT - 1) / (16 * MT);
     a.quads = (a.ins + 511) / 512;
@@ -501,7 +479,7 @@ static hipError_t launch_matvec(rh_ctx* ctx, matvec_args a)
         groups = groups < wgs ? groups : wgs;
         const int rounds = (a.tiles + groups * a.tw - 1) / (groups * a.tw), full = a.slice / a.chunk, rest = a.slice % a.chunk;
         const int depth = rounds * (full * ((a.chunk + a.ks - 1) / a.ks) + (rest + a.ks - 1) / a.ks);          // stretches a wave goes through
-        const float laid = (float)(K::PARTS * 512 * (16 / K::PIECE)) * M * a.slice * (whole ? 1 : rounds), read = (float)rounds * a.tw * R * 16 * 272 * a.slice;
+        const float laid = (float)(K::PARTS * 512 * 2) * M * a.slice * (whole ? 1 : rounds), read = (float)rounds * a.tw * R * 16 * 272 * a.slice;
         const float join = a.slices == 1 ? 0.f : (a.slices > 8 ? 3.9f : 2.9f) + 1.1e-6f * a.slices * gy * a.tiles * (R * MT * 1024.f);
         return 25e-6f * laid + 14e-6f * read + 1.7f * depth + join;
     };
@@ -524,7 +502,7 @@ static hipError_t launch_matvec(rh_ctx* ctx, matvec_args a)
     // waves, and as many more as have pieces of x to lay out, four a thread; two of fp32 rows, which are cut (16 x 1024 x 510: eight 7.7 us, four 6.5,
     // two 5.7; bf16 rows, 16 x 1024 x 512, 4.4, 4.3, 4.6, 64 x 1024 x 510 6.1, 5.5, 5.5)
     constexpr int SHARE = 64 * (XT == RH_T_F32 ? 2 : 4);
-    const int64_t pieces = (int64_t)a.chunk * (512 / K::PIECE) * M;
+    const int64_t pieces = (int64_t)a.chunk * (512 / MATVEC_PIECE) * M;
     int waves = a.tw * a.ks;
     while (waves < WAVES && (int64_t)waves * SHARE <= pieces) ++waves;
     a.threads = 64 * waves;
@@ -565,8 +543,6 @@ extern "C" rh_status rh_matvec_packed(rh_ctx* ctx, const void* x, int32_t x_type
     hipError_t e;
     if (x_type == RH_T_F32) e = launch_matvec<RH_T_F32, 1, 1>(ctx, a);
     else if (x_type == RH_T_BF16) e = n_rows <= 16 ? launch_matvec<RH_T_BF16, 1, 1>(ctx, a) : launch_matvec<RH_T_BF16, 2, 2>(ctx, a);
-    else if (y_type == RH_T_BF16 && n_in >= 512)
-        e = n_rows <= 16 ? launch_matvec<MATVEC_SCALED, 1, 1>(ctx, a) : n_rows <= 32 ? launch_matvec<MATVEC_SCALED, 2, 2>(ctx, a) : launch_matvec<MATVEC_SCALED, 4, 2>(ctx, a);
     else e = n_rows <= 16 ? launch_matvec<RH_T_E4M3, 1, 1>(ctx, a) : launch_matvec<RH_T_E4M3, 2, 2>(ctx, a);
     RH_HIP(ctx, e);
     return RH_OK;
