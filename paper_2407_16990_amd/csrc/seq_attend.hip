@@ -13,8 +13,8 @@
 //            the tokens in the order of the scores' registers; a lane loads E consecutive elements of each of its tokens, and the
 //            product's rows are taken as d = E*m + e for the E products of that load, so that a transposition inside the lane (a byte
 //            permutation for two 16-bit values, none for fp32) is all that the values need
-// A weight goes into the 16-bit product as the sum of two bf16 numbers: rounded to one, its error would be as large as the output's
-// own rounding.  An e4m3 key's scale multiplies its score, a value's scale its weight.
+// A weight goes into the 16-bit product as the sum of three bf16 numbers, which together are the weight exactly; they have its sign, so that an infinite
+// value gives the infinity that the weight gives, and not the NaN of two infinities.  An e4m3 key's scale multiplies its score, a value's scale its weight.
 //
 // Work is split over the streams' lengths: all streams' tiles (times the head units) are cut into chunks of equal size, so that a long stream
 // among short ones keeps every CU busy.  How long a chunk is follows from the lengths, which the host does not know: every
@@ -381,15 +381,28 @@ __global__ __launch_bounds__(ATTEND_T, D <= 128 ? 2 : 1) void k_seq_attend(atten
 #pragma unroll
                     for (int r = 0; r < ROWS; ++r) acc[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vr[r][i]), p[r], acc[i], 0, 0, 0);
             } else {
-                attend_words<4> hi, lo;
+                attend_words<4> part[3];
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
-                    float x = p[2 * w], y = p[2 * w + 1];
-                    if constexpr (KIND == RH_T_E4M3) { x *= vs[2 * w]; y *= vs[2 * w + 1]; }
-                    hi.w[w] = seq_pack_bf16(x, y);
-                    lo.w[w] = seq_pack_bf16(x - seq_bf16_lo(hi.w[w]), y - seq_bf16_hi(hi.w[w]));
+                    uint32_t cut[2][3];
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        float x = p[2 * w + h];
+                        if constexpr (KIND == RH_T_E4M3) x *= vs[2 * w + h];
+                        auto first = [](float v) { return __uint_as_float(__float_as_uint(v) & 0xFFFF0000u); };      // its eight leading bits
+                        const float hi = first(x);
+                        float r = x - hi;
+                        if constexpr (KIND == RH_T_E4M3) r = x == hi ? 0.f : r;           // an infinite scale; the values are finite
+                        // no part of a weight above zero is zero, or an infinite value would make it NaN
+                        else r = fmaxf(r, hi * 0x1p-30f);
+                        const float mid = first(r);
+                        float lo = r - mid;
+                        if constexpr (KIND == RH_T_BF16) lo = fmaxf(lo, hi * 0x1p-30f);
+                        cut[h][0] = __float_as_uint(hi); cut[h][1] = __float_as_uint(mid); cut[h][2] = __float_as_uint(lo);
+                    }
+#pragma unroll
+                    for (int k = 0; k < 3; ++k) part[k].w[w] = __builtin_amdgcn_perm(cut[1][k], cut[0][k], 0x07060302u);
                 }
-                const bf16x8 ph = __builtin_bit_cast(bf16x8, hi), pl = __builtin_bit_cast(bf16x8, lo);
 #pragma unroll
                 for (int i = 0; i < NT; i += 2) {
                     attend_words<4> even, odd;
@@ -405,10 +418,12 @@ __global__ __launch_bounds__(ATTEND_T, D <= 128 ? 2 : 1) void k_seq_attend(atten
                         odd.w[w] = __builtin_amdgcn_perm(y, x, 0x07060302u);
                     }
                     const bf16x8 va = __builtin_bit_cast(bf16x8, even), vb = __builtin_bit_cast(bf16x8, odd);
-                    acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, ph, acc[i], 0, 0, 0);
-                    acc[i + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vb, ph, acc[i + 1], 0, 0, 0);
-                    acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, pl, acc[i], 0, 0, 0);
-                    acc[i + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vb, pl, acc[i + 1], 0, 0, 0);
+#pragma unroll
+                    for (int k = 2; k >= 0; --k) {
+                        const bf16x8 pw = __builtin_bit_cast(bf16x8, part[k]);
+                        acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, pw, acc[i], 0, 0, 0);
+                        acc[i + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vb, pw, acc[i + 1], 0, 0, 0);
+                    }
                 }
             }
             if constexpr (MORE) {
