@@ -7,12 +7,12 @@
 //   fp32 rows   the same against x cut into three bf16 parts, which together are x exactly: products of full precision at three
 //               products of the 16-bit rate, where the fp32 rate is a sixteenth of it
 //   e4m3 rows   as bf16 rows, which hold them exactly.  (The scaled product of 8-bit and 4-bit values would take codes, scales and rows as they
-//               are - 10.1 us for the 12.5 below - but keeps fewer than 32 bits of its partial sums: two pairs of +-448 that cancel in a row of 8192 small terms
+//               are - 10.1 us for 16 x 16384 x 4096 - but keeps fewer than 32 bits of its partial sums: two pairs of +-448 that cancel in a row of 8192 small terms
 //               left 1.2 where the sum is -0.03.)
 // A workgroup's waves share out its tiles of outputs and the inner index (KS waves a tile, summed in LDS in order), so that few outputs
 // still use every wave; where x is long or the tiles are few, workgroups share the inner index too, and the last of them adds up their sums, in their order.
-// 16 x 16384 x 4096, e4m3 rows: 12.5 us, 2.9 TB/s of weights; 7.0 at a copy's rate, about 2 until the first bytes are there, the rest x.  1 x 1024 x 510,
-// fp32: 4.0, hardly more than an empty launch (2.5) and one way to memory.
+// 16 x 16384 x 4096, e4m3 rows: 11.6 us, 3.1 TB/s of weights; 7.0 at a copy's rate, about 2 until the first bytes are there, the rest x.  1 x 1024 x 510,
+// fp32: 4.1, hardly more than an empty launch (2.5) and one way to memory.
 #include "seq_common.h"
 
 struct matvec_args {
@@ -65,23 +65,12 @@ __device__ __forceinline__ bf16x8 matvec_wide(uint32_t c, uint32_t scale)
     r.two[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, f, 3);
     return r.all;
 }
-// the same by 2^-8, which keeps every code of every scale finite; a scale of 255 is not a number
-__device__ __forceinline__ bf16x8 matvec_wide_slow(uint32_t c, uint32_t scale)
+// The value of a code without its block's scale
+__device__ __forceinline__ float matvec_code(uint32_t code)
 {
-    union { uint32_t w[4]; bf16x8 all; } r;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        float v[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const uint32_t code = c >> (8 * i + 4 * h) & 15, m = code & 7;
-            float f = m < 2 ? 0.5f * (float)m : __uint_as_float((126 + (m >> 1)) << 23 | (m & 1) << 22);
-            f *= scale == 255 ? __builtin_nanf("") : scale > 8 ? __uint_as_float((scale - 8) << 23) : 0.f;
-            v[h] = code & 8 ? -f : f;
-        }
-        r.w[i] = seq_pack_bf16(v[0], v[1]);
-    }
-    return r.all;
+    const uint32_t m = code & 7;
+    const float f = m < 2 ? 0.5f * (float)m : __uint_as_float((126 + (m >> 1)) << 23 | (m & 1) << 22);
+    return code & 8 ? -f : f;
 }
 
 // SPLIT: the inner index is cut into slices; ENDS: it is no multiple of 512 (what the others need not look at costs them up to 0.8 us of 14)
@@ -277,28 +266,48 @@ __global__ __launch_bounds__(64 * MATVEC_WAVES(XT, MT)) void k_seq_matvec(matvec
                         }
                 }
             } else {
-                // codes that bf16 cannot hold: this step's products by 2^-8, on their own
-                f32x4 part[R][MT];
-#pragma unroll
-                for (int r = 0; r < R; ++r)
-#pragma unroll
-                    for (int i = 0; i < MT; ++i) part[r][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+                // A block whose codes bf16 cannot hold: this step a term at a time in 32 bits, where blocks of any other scale keep their values beside it.  Terms of
+                // such blocks are summed by 2^-8.  The lane that has output 4*j + e of a product has its block b's codes in lane 16*b + 4*j + e.  (Seldom
+                // or never reached: written for few registers.)
 #pragma unroll 1
-                for (int e = 0; e < 4; ++e)
+                for (int e = 0; e < 4; ++e) {
+                    float plain[R][MT] = {}, huge8[R][MT] = {};
+#pragma unroll 1
+                    for (int at = 0; at < 16; ++at) {
+                        const int b = at >> 2, e8 = at & 3;  // block, and eight of its codes
+                        uint32_t code[R], by[R];
 #pragma unroll
-                    for (int r = 0; r < R; ++r) {
-                        const uint32_t code = e == 0 ? w.code[r][s][0] : e == 1 ? w.code[r][s][1] : e == 2 ? w.code[r][s][2] : w.code[r][s][3];
-                        const bf16x8 wa = matvec_wide_slow(code, scale[r]);
+                        for (int r = 0; r < R; ++r) {
+                            const u32x4 all = w.code[r][s];
+                            code[r] = (uint32_t)__shfl((int)(e8 == 0 ? all[0] : e8 == 1 ? all[1] : e8 == 2 ? all[2] : all[3]), 16 * b + 4 * j + e);
+                            by[r] = (uint32_t)__shfl((int)scale[r], 16 * b + 4 * j + e);
+                        }
+#pragma unroll 1
+                        for (int n = 0; n < 8; ++n) {
 #pragma unroll
-                        for (int p = PARTS - 1; p >= 0; --p)
+                            for (int i = 0; i < MT; ++i) {
+                                float v = 0.f;
 #pragma unroll
-                            for (int i = 0; i < MT; ++i)
-                                part[r][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wa, __builtin_bit_cast(bf16x8, x[p * part_pieces + e * 4 * P + mrow[i]]), part[r][i], 0, 0, 0);
+                                for (int p = PARTS - 1; p >= 0; --p)
+                                    v += __uint_as_float((uint32_t)((const uint16_t*)&x[p * part_pieces + (e8 * 4 + b) * P + mrow[i] - j * P])[n] << 16);
+#pragma unroll
+                                for (int r = 0; r < R; ++r) {
+                                    const bool is_huge = by[r] >= MATVEC_HUGE;
+                                    const float f = by[r] == 255 ? __builtin_nanf("") : matvec_code(code[r] >> (4 * n));
+                                    const float term = __builtin_amdgcn_ldexpf(f * v, (int)by[r] - (is_huge ? 135 : 127));
+                                    plain[r][i] += is_huge ? 0.f : term;
+                                    huge8[r][i] += is_huge ? term : 0.f;
+                                }
+                            }
+                        }
                     }
 #pragma unroll
-                for (int r = 0; r < R; ++r)
+                    for (int r = 0; r < R; ++r)
 #pragma unroll
-                    for (int i = 0; i < MT; ++i) acc[r][i] += part[r][i] * 256.f;
+                        for (int i = 0; i < MT; ++i)
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) acc[r][i][k] += k == e ? plain[r][i] + huge8[r][i] * 256.f : 0.f;
+                }
             }
         }
     };

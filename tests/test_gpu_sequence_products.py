@@ -73,3 +73,51 @@ def test_rows_of_8_bits_with_bf16_outputs(rh, rows, n_out, n_in):  # noqa: F811
     assert bool(z[rows // 2].isnan().all())
     z[rows // 2] = y[rows // 2]
     assert torch.equal(z, y)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,n_out,n_in", [(1, 48, 32), (2, 100, 130), (17, 90, 512), (33, 64, 700), (64, 200, 2048), (16, 60, 16384)])
+def test_outputs_of_scales_far_apart_side_by_side(rh, dtype, rows, n_out, n_in):  # noqa: F811
+    """Neighbouring outputs whose blocks have the smallest scales, the largest and others: each comes out as it would alone.  Rows of two sizes, for the
+    large scales and for the small ones (8-bit rows cannot be that far apart)."""
+    rng = np.random.default_rng(n_in + rows)
+    g = torch.Generator(device="cuda").manual_seed(n_in)
+    w, _ = _weights(g, n_out, n_in)
+    blocks = (n_in + 31) // 32
+    scales = np.array([2, 3, 8, 9, 60, 127, 200, 251, 252, 253, 254], dtype=np.uint8)
+    small, large = 2.0 ** -20, 2.0 ** 60
+    for mixed in (False, True):
+        # one scale an output, or two a row: the small beside the large of the same output
+        sc = np.repeat(rng.choice(scales, (n_out, 1)), blocks, axis=1)
+        if mixed:
+            sc = np.where(rng.random((n_out, blocks)) < 0.5, sc, rng.choice(scales, (n_out, blocks)))
+        x = rng.standard_normal((rows, n_in)) * (small if dtype != E4M3 else 2.0 ** -4)
+        if dtype != E4M3:
+            x[1::2] *= large / small
+        t = torch.from_numpy(x).float().to(dtype).cuda()
+        xn = t.double().cpu().numpy() if dtype != E4M3 else S.e4m3_values()[t.view(torch.uint8).cpu().numpy()]
+        d_sc = torch.from_numpy(sc.astype(np.uint8)).cuda()
+        real = S.unpack_weights(w.cpu().numpy(), sc.astype(np.uint8), n_in)
+        want, most = xn @ real.T, np.abs(xn) @ np.abs(real).T
+        y = rh.matvec_packed(t, w, d_sc, out_dtype=torch.float32).double().cpu().numpy()
+        held = most < 2.0 ** 127                                   # others' partial sums may pass fp32
+        tol = (n_in + 8) * 2.0 ** -24 * most + 2.0 ** -24 * np.abs(want) + n_in * 2.0 ** -149
+        assert mixed or held.any()
+        assert (np.abs(y - want)[held] <= tol[held]).all(), np.argwhere(held & ~(np.abs(y - want) <= tol))[:5]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows,n_in", [(1, 32), (18, 512), (33, 600)])
+def test_infinite_inputs_beside_the_largest_scales(rh, dtype, rows, n_in):  # noqa: F811
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    w, _ = _weights(g, 64, n_in)
+    blocks = (n_in + 31) // 32
+    sc = torch.full((64, blocks), 120, dtype=torch.uint8, device="cuda")
+    sc[5], sc[20, blocks // 2], sc[41] = 253, 254, 3
+    x = (torch.randn((rows, n_in), generator=g, device="cuda") * 2.0 ** -20).to(dtype)
+    x[rows // 2, n_in // 2] = float("inf")
+    y = rh.matvec_packed(x, w, sc, out_dtype=torch.float32).double().cpu().numpy()
+    with np.errstate(invalid="ignore"):
+        want = np.stack([(row * S.unpack_weights(w.cpu().numpy(), sc.cpu().numpy(), n_in)).sum(-1) for row in x.double().cpu().numpy()])
+    bad = ~np.isfinite(want)
+    assert bad.sum() == 64 and np.array_equal(y[bad], want[bad], equal_nan=True) and np.isfinite(y[~bad]).all()
