@@ -115,7 +115,7 @@ class StreamPredictor:
 
     def step(self, features: torch.Tensor, n_new: torch.Tensor) -> torch.Tensor:
         """features f32 [max_streams, n_features], n_new int32 [max_streams]: 1 - a frame of this stream, 0 - none, -1 - the
-        stream has ended -> scores f32 [max_streams, mbh, mbw], of the streams with a frame.  A stream that got no room in the
+        stream has ended -> scores f32 [max_streams, mbh, mbw], of the streams with a frame; a tensor of its own every time.  A stream that got no room in the
         cache (its length stays) is scored from the frames that it has."""
         self.features.copy_(features)
         self.n_new.copy_(n_new)
@@ -125,7 +125,7 @@ class StreamPredictor:
         if self.graph is None:
             return self._step()
         self.graph.replay()
-        return self.scores
+        return self.scores.clone()                                 # the graph's own tensor is the next step's too
 
     def _record(self):
         rh, main = self.rh, self.rh._stream
