@@ -12,7 +12,9 @@
  * stream, arguments checked before any launch, rh_last_error.  They use neither the context's network nor its capacities,
  * and count in no class of rh_profile_read.  Sums, softmax statistics and norms are held in 32 bits.
  * Scratch memory of rh_cache_attend and rh_matvec_packed (68 MB on 256 CUs) and a few counters, of rh_cache_plan too, belong to the context: the first call that wants
- * them allocates them, no later one allocates or synchronises, so that from then on calls may be captured into graphs.
+ * them allocates them and waits for the stream, and no later one does.  Graphs may be recorded once an rh_cache_attend or rh_matvec_packed call of the context has been made
+ * (RH_E_STATE where a captured call would have to allocate).  Since calls share this memory, those of one context must not overlap on two streams, replays of
+ * a graph that recorded them among them: use a context for each, or let one wait for the other.
  */
 #ifndef RH_SEQ_H
 #define RH_SEQ_H

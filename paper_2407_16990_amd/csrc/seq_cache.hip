@@ -363,22 +363,39 @@ __global__ void k_seq_zero(uint32_t* p, uint32_t n)
     if (i < n) p[i] = 0;
 }
 
-// Both are made once, at their full size, at the first call that wants them: what a graph has recorded stays where it is.
+// Both are made once, at their full size, at the first call that wants them: what a graph has recorded stays where it is.  Not while the stream is being captured, where the
+// fill of the counters would only be recorded, and calls ahead of the first replay would count from whatever is there.
+static rh_status seq_may_allocate(rh_ctx* ctx)
+{
+    hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+    const hipError_t e = hipStreamIsCapturing(ctx->stream, &capture);
+    if (e == hipErrorStreamCaptureImplicit || (e == hipSuccess && capture != hipStreamCaptureStatusNone))
+        RH_FAIL(ctx, RH_E_STATE, "the sequence operators' memory is not there yet and cannot be allocated in a stream capture: make one such call before it");
+    return RH_OK;
+}
+
 rh_status seq_counters(rh_ctx* ctx)
 {
     if (ctx->seq_cnt) return RH_OK;
+    const rh_status st = seq_may_allocate(ctx);
+    if (st != RH_OK) return st;
     const uint32_t n = (uint32_t)SEQ_ROWS(ctx);
-    if (hipMalloc((void**)&ctx->seq_cnt, n * sizeof(uint32_t)) != hipSuccess) { ctx->seq_cnt = nullptr; RH_FAIL(ctx, RH_E_NOMEM, "%u counters", n); }
-    // A fill kernel that was lost leaves no counters behind: the next call would trust them to be zero.
-    hipLaunchKernelGGL(k_seq_zero, dim3((n + 255) / 256), dim3(256), 0, ctx->stream, ctx->seq_cnt, n);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) { (void)hipFree(ctx->seq_cnt); ctx->seq_cnt = nullptr; RH_FAIL(ctx, RH_E_DEVICE, "clearing counters: %s", hipGetErrorString(e)); }
+    uint32_t* made = nullptr;
+    if (hipMalloc((void**)&made, n * sizeof(uint32_t)) != hipSuccess) RH_FAIL(ctx, RH_E_NOMEM, "%u counters", n);
+    // The context has them once they are zero: the next call may be on another stream, and one behind a lost fill would trust them.
+    hipLaunchKernelGGL(k_seq_zero, dim3((n + 255) / 256), dim3(256), 0, ctx->stream, made, n);
+    hipError_t e = hipGetLastError();
+    if (e == hipSuccess) e = hipStreamSynchronize(ctx->stream);
+    if (e != hipSuccess) { (void)hipFree(made); RH_FAIL(ctx, RH_E_DEVICE, "clearing counters: %s", hipGetErrorString(e)); }
+    ctx->seq_cnt = made;
     return RH_OK;
 }
 
 rh_status seq_scratch(rh_ctx* ctx)
 {
     if (ctx->seq_ws) return RH_OK;
+    const rh_status st = seq_may_allocate(ctx);
+    if (st != RH_OK) return st;
     const size_t bytes = (size_t)SEQ_ROWS(ctx) * SEQ_ROW_BYTES(RH_SEQ_MAX_DIM);
     if (hipMalloc(&ctx->seq_ws, bytes) != hipSuccess) { ctx->seq_ws = nullptr; RH_FAIL(ctx, RH_E_NOMEM, "scratch memory of %zu bytes", bytes); }
     return RH_OK;
