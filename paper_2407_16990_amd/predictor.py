@@ -34,7 +34,8 @@ class PredictorConfig:
     page: int = 16              # frames a page of the cache
     n_pages: int = 4096         # of all streams together
     max_pages: int = 512        # of one stream
-    window: int = 0             # frames that attention looks back; 0: all
+    window: int = 0             # frames that attention looks back; 0: all.  Pages behind it are given back, so that a stream goes on for ever where
+                                # window + page <= max_pages * page; without a window it has room for max_pages * page frames
     eps: float = 1e-6
     cache_dtype: torch.dtype = torch.bfloat16      # or torch.float8_e4m3fn
 
@@ -58,7 +59,9 @@ def random_weights(cfg: PredictorConfig, seed: int) -> dict:
 
 class StreamPredictor:
     """The state of max_streams streams and the step that takes one frame of each.  rh: the context whose stream the work goes
-    on, and which is to be torch's current one.  graph: record the step at its second call and replay it from then on (one launch instead of one per operator)."""
+    on, and which is to be torch's current one; other calls of that context must not overlap with a step on another stream, replays included.
+    graph: record the step at its second call and replay it from then on (one launch instead of one per operator).
+    lengths: frames of each stream that found room since it began; granted: which streams' frames did in the last step."""
 
     def __init__(self, rh: RH, cfg: PredictorConfig, weights: dict, graph: bool = False):
         self.rh, self.cfg, dev = rh, cfg, rh.device
@@ -80,9 +83,11 @@ class StreamPredictor:
         n = cfg.max_streams
         i32 = dict(dtype=torch.int32, device=dev)
         self.lengths, self.table = torch.zeros(n, **i32), torch.full((n, cfg.max_pages), -1, **i32)
+        # frames in the cache: fewer than a stream has had once pages behind the window are given back
+        self.held, self.ended = (torch.zeros(n, **i32), torch.full((n,), -1, **i32)) if cfg.window else (self.lengths, None)
         self.free, self.free_count = torch.arange(cfg.n_pages, **i32), torch.full((1,), cfg.n_pages, **i32)
         self.features, self.n_new = torch.zeros((n, cfg.n_features), device=dev), torch.zeros(n, **i32)
-        self.want_graph, self.graph, self.scores, self.calls = graph, None, None, 0
+        self.want_graph, self.graph, self.outputs, self.calls, self.granted = graph, None, None, 0, None
 
     def _product(self, name, x, x_scale=None, **kw):
         return self.rh.matvec_packed(x, *self.packed[name], x_scale=x_scale, **kw)
@@ -90,23 +95,38 @@ class StreamPredictor:
     def _step(self):
         rh, cfg = self.rh, self.cfg
         n, hq, hk, d = cfg.max_streams, cfg.q_heads, cfg.kv_heads, cfg.dim
-        slots, off, _, _ = rh.cache_plan(self.n_new, self.lengths, self.table, self.free, self.free_count, cfg.page, n,
-                                         new_lengths=self.lengths, new_count=self.free_count)
+        if cfg.window:
+            self._give_back()
+        slots, off, _, _ = rh.cache_plan(self.n_new, self.held, self.table, self.free, self.free_count, cfg.page, n,
+                                         new_lengths=self.held, new_count=self.free_count)
+        granted = off[1:] > off[:-1]
+        if cfg.window:
+            self.lengths.add_(granted).masked_fill_(self.n_new < 0, 0)
         # the plan lists tokens, the rows below are streams: a stream without a token in this step writes nothing
         mine = slots[off[:-1].clamp_max(n - 1).long()]
-        slots = torch.where(off[1:] > off[:-1], mine, torch.full_like(mine, -1))
+        slots = torch.where(granted, mine, torch.full_like(mine, -1))
         x = self._product("in", self.features, out_dtype=torch.bfloat16)
         h = None
         for i, cache in enumerate(self.caches):
             h, _, y, ys = self._norm(f"norm_a{i}", x, h)
             row = self._product(f"qkv{i}", y, ys)
             rh.cache_write(cache, row[:, hq * d:(hq + hk) * d].unflatten(1, (hk, d)), row[:, (hq + hk) * d:].unflatten(1, (hk, d)), slots)
-            a = rh.cache_attend(row[:, : hq * d].unflatten(1, (hq, d)), cache, self.table, self.lengths, window=cfg.window)
+            a = rh.cache_attend(row[:, : hq * d].unflatten(1, (hq, d)), cache, self.table, self.held, window=cfg.window)
             x = self._product(f"proj{i}", a.view(n, hq * d))
             h, _, y, ys = self._norm(f"norm_b{i}", x, h)
             x = self._product(f"narrow{i}", self._product(f"wide{i}", y, ys, relu=True))
         _, _, y, ys = self._norm("norm_out", x, h)
-        return self._product("out", y, ys, out_dtype=torch.float32).view(n, cfg.mbh, cfg.mbw)
+        return self._product("out", y, ys, out_dtype=torch.float32).view(n, cfg.mbh, cfg.mbw), granted
+
+    def _give_back(self):
+        """The first page of every stream whose frames there all lie behind the window (a step adds one frame, so that one page a step is
+        enough): on the free stack as the page of a stream that has ended, and out of the stream's row of the table."""
+        cfg = self.cfg
+        drop = self.held >= cfg.window + cfg.page
+        frames = drop.int() * cfg.page
+        self.rh.cache_plan(self.ended, frames, self.table[:, :1].contiguous(), self.free, self.free_count, cfg.page, 1, new_count=self.free_count)
+        self.table[:, :-1] = torch.where(drop[:, None], self.table[:, 1:], self.table[:, :-1])
+        self.held.sub_(frames)
 
     def _norm(self, name, x, h):
         """The residual stream with x added to it (x itself begins it), and the norm of it in 8 bits."""
@@ -116,16 +136,18 @@ class StreamPredictor:
     def step(self, features: torch.Tensor, n_new: torch.Tensor) -> torch.Tensor:
         """features f32 [max_streams, n_features], n_new int32 [max_streams]: 1 - a frame of this stream, 0 - none, -1 - the
         stream has ended -> scores f32 [max_streams, mbh, mbw], of the streams with a frame; a tensor of its own every time.  A stream that got no room in the
-        cache (its length stays) is scored from the frames that it has."""
+        cache (`granted` is False there, its length stays) is scored from the frames that it has: end it and begin it anew, or give the cache more room."""
         self.features.copy_(features)
         self.n_new.copy_(n_new)
         self.calls += 1
         if self.graph is None and self.want_graph and self.calls > 1:
             self._record()
         if self.graph is None:
-            return self._step()
+            scores, self.granted = self._step()
+            return scores
         self.graph.replay()
-        return self.scores.clone()                                 # the graph's own tensor is the next step's too
+        scores, self.granted = (t.clone() for t in self.outputs)   # the graph's own tensors are the next step's too
+        return scores
 
     def _record(self):
         rh, main = self.rh, self.rh._stream
@@ -133,7 +155,7 @@ class StreamPredictor:
         rh.set_stream(side)
         try:
             with torch.cuda.graph(graph, stream=side):
-                self.scores = self._step()
+                self.outputs = self._step()
         finally:
             rh.set_stream(main)
         self.graph = graph
