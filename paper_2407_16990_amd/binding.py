@@ -56,14 +56,35 @@ def lib_path() -> str:
 
 
 _lib = None
-_seq = None            # _seq.so: the sequence operators on torch tensors (csrc/seq_binding.cpp)
+
+
+class _Sequence:
+    """_seq.so, the sequence operators on torch tensors (csrc/seq_binding.cpp), loaded when one is first called: what else the library
+    does needs neither it nor a host compiler.  It is built first when it is missing, or made from other sources or for another torch or Python."""
+
+    def __getattr__(self, name):
+        if name.startswith("__"):
+            raise AttributeError(name)
+        from . import build as _b
+        L = load_library()
+        if _b.module_is_stale():
+            _b.build_module()
+        spec = importlib.util.spec_from_file_location("_seq", _b.MODULE)
+        module = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(module)
+        module.init(*[C.cast(f, C.c_void_p).value for f in (L.rh_cache_plan, L.rh_cache_write, L.rh_cache_attend, L.rh_norm_residual, L.rh_matvec_packed)])
+        self.__dict__.update({n: f for n, f in vars(module).items() if not n.startswith("__")})        # from here on without this function
+        return self.__dict__[name]
+
+
+_seq = _Sequence()
 
 
 def _library_is_stale(path: str) -> bool:
     """True when librh.so is missing or was built from other sources than the ones in the tree
     (build.py records a digest of csrc/ and include/ beside the library)."""
     from . import build as _b
-    if not os.path.exists(path) or not os.path.exists(_b.STAMP) or not os.path.exists(_b.MODULE):
+    if not os.path.exists(path) or not os.path.exists(_b.STAMP):
         return True
     with open(_b.STAMP) as f:
         return f.read().strip() != _b.source_digest()
@@ -71,13 +92,13 @@ def _library_is_stale(path: str) -> bool:
 
 def load_library():
     """Load librh.so; it is built first when it is missing or a source file is newer than it."""
-    global _lib, _seq
+    global _lib
     if _lib is not None:
         return _lib
     path = lib_path()
     if _library_is_stale(path):
         from . import build as _b
-        _b.build()
+        _b.build_library()
     L = C.CDLL(path)
     vp, i32 = C.c_void_p, C.c_int32
     L.rh_budget.restype = C.c_uint32
@@ -111,10 +132,6 @@ def load_library():
     L.rh_norm_residual.argtypes = [vp, vp, i64, vp, i64, vp, i32, i32, i32, f32, vp, i64, vp, vp, vp]
     L.rh_matvec_packed.argtypes = [vp, vp, i32, i64, vp, vp, vp, i32, i32, i32, i32, vp, i32, i64]
     L.rh_select_regions_noalloc.argtypes = [vp, i32, i32, i32, C.POINTER(Segment), i32, i32, vp, vp, vp, vp]
-    spec = importlib.util.spec_from_file_location("_seq", os.path.join(_HERE, "_seq.so"))
-    _seq = importlib.util.module_from_spec(spec)
-    spec.loader.exec_module(_seq)
-    _seq.init(*[C.cast(f, vp).value for f in (L.rh_cache_plan, L.rh_cache_write, L.rh_cache_attend, L.rh_norm_residual, L.rh_matvec_packed)])
     _lib = L
     return L
 
@@ -167,8 +184,6 @@ class KVCache:
     [n_pages, heads, page] for float8_e4m3fn, else None."""
 
     def __init__(self, k, v, k_scale=None, v_scale=None):
-        if _seq is None:
-            load_library()
         self.desc = _seq.kv_desc(k, v, k_scale, v_scale)           # rh_kv_cache
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
 

@@ -21,6 +21,7 @@ MODULE = os.path.join(HERE, "_seq.so")
 MODULE_SOURCE = "seq_binding.cpp"
 MODULE_FLAGS = ["-std=c++17", "-O2", "-fPIC", "-shared", "-Wall"]
 STAMP = LIB + ".sources"      # digest of the sources the library was built from
+MODULE_STAMP = MODULE + ".sources"
 SOURCES = ["rh_api.hip", "select.hip", "plan.hip", "pack.hip", "unpack.hip", "conv_fp32.hip", "conv_mfma.hip",
            "conv_mfma_duo.hip", "conv_body.hip", "conv_block32.hip", "conv_block64.hip", "conv_tail.hip", "conv_head.hip", "conv_fold.hip", "conv_mask.hip", "temporal.hip", "noalloc.hip",
            "seq_cache.hip", "seq_norm.hip", "seq_attend.hip", "seq_matvec.hip"]
@@ -43,7 +44,13 @@ def _headers():
 
 def source_digest() -> str:
     """SHA-256 over the names and contents of every file the library is compiled from."""
-    return _digest([os.path.join(CSRC, s) for s in SOURCES + [MODULE_SOURCE]] + _headers(), " ".join(FLAGS + MODULE_FLAGS))
+    return _digest([os.path.join(CSRC, s) for s in SOURCES] + _headers(), " ".join(FLAGS))
+
+
+def module_digest() -> str:
+    """The same of _seq.so, and what its C++ interface depends on: torch and its ABI, and Python."""
+    import torch
+    return _digest([os.path.join(CSRC, MODULE_SOURCE)] + _headers(), f"{MODULE_FLAGS} {torch.__version__} {torch._C._GLIBCXX_USE_CXX11_ABI} {sys.version}")
 
 
 SETTLED = 20       # wait states from a matrix product to a vector instruction that reads its sums, more than any product needs
@@ -129,38 +136,43 @@ def _compile(hipcc: str, src: str, force: bool):
     return obj, r.stdout + r.stderr
 
 
-def _compile_module(force: bool) -> str:
+def module_is_stale() -> bool:
+    """True when _seq.so is missing, or was built from other sources or for another torch or Python."""
+    if not os.path.exists(MODULE) or not os.path.exists(MODULE_STAMP):
+        return True
+    with open(MODULE_STAMP) as f:
+        return f.read().strip() != module_digest()
+
+
+def build_module(force: bool = False) -> str:
     """_seq.so, by the host compiler, against the headers of the installed torch."""
     import sysconfig
 
     import torch
-    src, root = os.path.join(CSRC, MODULE_SOURCE), os.path.dirname(torch.__file__)
-    tag = _digest([src] + _headers(), " ".join(MODULE_FLAGS) + torch.__version__ + sys.version)
-    tag_file = os.path.join(OBJ, MODULE_SOURCE + ".tag")
-    if not force and os.path.exists(MODULE) and os.path.exists(tag_file) and open(tag_file).read() == tag:
+    if not force and not module_is_stale():
         return ""
+    src, root, made = os.path.join(CSRC, MODULE_SOURCE), os.path.dirname(torch.__file__), f"{MODULE}.{os.getpid()}"
     cmd = [os.environ.get("CXX", "g++")] + MODULE_FLAGS + [f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I" + INCLUDE]
     for d in (os.path.join(root, "include"), os.path.join(root, "include", "torch", "csrc", "api", "include"), sysconfig.get_paths()["include"]):
         cmd += ["-isystem", d]
-    cmd += [src, "-o", MODULE, "-L" + os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"]
+    cmd += [src, "-o", made, "-L" + os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError(f"{cmd[0]} failed on {MODULE_SOURCE}:\n{r.stdout}{r.stderr}")
-    with open(tag_file, "w") as f:
-        f.write(tag)
+    os.replace(made, MODULE)
+    with open(MODULE_STAMP, "w") as f:
+        f.write(module_digest() + "\n")
     return r.stdout + r.stderr
 
 
-def build(verbose: bool = False, force: bool = False) -> str:
+def build_library(verbose: bool = False, force: bool = False) -> str:
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     os.makedirs(OBJ, exist_ok=True)
     jobs = min(8, int(os.environ.get("MAX_JOBS", "8")), len(SOURCES))
     with ThreadPoolExecutor(jobs) as ex:
-        module = ex.submit(_compile_module, force)
         res = list(ex.map(lambda s: _compile(hipcc, s, force), SOURCES))
-        res_module = module.result()
     if verbose:
-        sys.stderr.write("".join(log for _, log in res) + res_module)
+        sys.stderr.write("".join(log for _, log in res))
     r = subprocess.run([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB] + [o for o, _ in res],
                        capture_output=True, text=True)
     if verbose or r.returncode != 0:
@@ -170,6 +182,17 @@ def build(verbose: bool = False, force: bool = False) -> str:
     with open(STAMP, "w") as f:
         f.write(source_digest() + "\n")
     return LIB
+
+
+def build(verbose: bool = False, force: bool = False) -> str:
+    """Both."""
+    with ThreadPoolExecutor(1) as ex:
+        module = ex.submit(build_module, force)
+        lib = build_library(verbose, force)
+        log = module.result()
+    if verbose:
+        sys.stderr.write(log)
+    return lib
 
 
 if __name__ == "__main__":
