@@ -181,27 +181,20 @@ _raw_stream = torch._C._cuda_getCurrentRawStream     # handle of torch's current
 class KVCache:
     """A paged cache of keys and values: k, v [n_pages, page, heads, dim] (any strides whose last is 1, in multiples of
     16 bytes: a [n_pages, heads, page, dim] tensor goes in transposed); k_scale, v_scale f32
-    [n_pages, heads, page] for float8_e4m3fn, else None."""
+    [n_pages, heads, page] for float8_e4m3fn, else None.  It holds on to these tensors and where they lie: they are not replaced, another cache is made."""
 
     def __init__(self, k, v, k_scale=None, v_scale=None):
         self.desc = _seq.kv_desc(k, v, k_scale, v_scale)           # rh_kv_cache
-        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self._tensors = (k, v, k_scale, v_scale)
 
-    @property
-    def n_pages(self) -> int:
-        return self.k.shape[0]
-
-    @property
-    def page(self) -> int:
-        return self.k.shape[1]
-
-    @property
-    def heads(self) -> int:
-        return self.k.shape[2]
-
-    @property
-    def dim(self) -> int:
-        return self.k.shape[3]
+    k = property(lambda self: self._tensors[0])
+    v = property(lambda self: self._tensors[1])
+    k_scale = property(lambda self: self._tensors[2])
+    v_scale = property(lambda self: self._tensors[3])
+    n_pages = property(lambda self: self.k.shape[0])
+    page = property(lambda self: self.k.shape[1])
+    heads = property(lambda self: self.k.shape[2])
+    dim = property(lambda self: self.k.shape[3])
 
 
 def pack_weights(w) -> tuple:
