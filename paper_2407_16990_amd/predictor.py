@@ -65,6 +65,8 @@ class StreamPredictor:
 
     def __init__(self, rh: RH, cfg: PredictorConfig, weights: dict, graph: bool = False):
         self.rh, self.cfg, dev = rh, cfg, rh.device
+        if cfg.cache_dtype not in (torch.bfloat16, torch.float8_e4m3fn):
+            raise ValueError(f"cache_dtype {cfg.cache_dtype}: keys and values are bf16, the cache torch.bfloat16 or torch.float8_e4m3fn")
         for name, shape in weight_shapes(cfg).items():
             if tuple(weights[name].shape) != shape:
                 raise ValueError(f"{name}: {tuple(weights[name].shape)}, not {shape}")
