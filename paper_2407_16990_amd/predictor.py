@@ -97,6 +97,7 @@ class StreamPredictor:
     def _step(self):
         rh, cfg = self.rh, self.cfg
         n, hq, hk, d = cfg.max_streams, cfg.q_heads, cfg.kv_heads, cfg.dim
+        self.n_new.clamp_(-1, 1)                                   # a step has one row a stream: no room is planned for more than it writes
         if cfg.window:
             self._give_back()
         slots, off, _, _ = rh.cache_plan(self.n_new, self.held, self.table, self.free, self.free_count, cfg.page, n,
@@ -136,7 +137,7 @@ class StreamPredictor:
         return (x if h is None else total), None, y, ys
 
     def step(self, features: torch.Tensor, n_new: torch.Tensor) -> torch.Tensor:
-        """features f32 [max_streams, n_features], n_new int32 [max_streams]: 1 - a frame of this stream, 0 - none, -1 - the
+        """features f32 [max_streams, n_features], n_new int32 [max_streams]: 1 (or more) - a frame of this stream, 0 - none, -1 (or less) - the
         stream has ended -> scores f32 [max_streams, mbh, mbw], of the streams with a frame; a tensor of its own every time.  A stream that got no room in the
         cache (`granted` is False there, its length stays) is scored from the frames that it has: end it and begin it anew, or give the cache more room."""
         self.features.copy_(features)

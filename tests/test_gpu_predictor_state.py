@@ -91,3 +91,16 @@ def test_frames_without_room_are_told(graph, max_pages, n_pages):
     pred.step(frames[8], ended)
     pred.step(frames[9], _ones(cfg))
     assert bool(pred.granted[0]) and int(pred.lengths[0]) == 1
+
+
+@pytest.mark.parametrize("graph", [False, True])
+def test_a_step_takes_one_frame_a_stream(graph):
+    """Numbers above one count as one: nothing is planned, and later read, that the step does not write."""
+    cfg = _config()
+    weights = P.random_weights(cfg, 4)
+    a, b = P.StreamPredictor(_rh(4), cfg, weights, graph=graph), P.StreamPredictor(_rh(4), cfg, weights)
+    for t, f in enumerate(_frames(cfg, 6)):
+        many = torch.tensor([1, 2, 7, -3 if t == 3 else 1], dtype=torch.int32, device="cuda")
+        x, y = a.step(f, many), b.step(f, many.clamp(-1, 1))
+        assert torch.equal(x[many > 0], y[many > 0]) and torch.equal(a.lengths, b.lengths) and torch.equal(a.granted, b.granted)
+    assert a.lengths.tolist() == [6, 6, 6, 2]
