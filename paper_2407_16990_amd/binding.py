@@ -249,12 +249,12 @@ class RH:
         if st != 0:
             raise RhError(st, "rh_create failed (see include/rh.h for the limits)")
         self.h = h
-        self._ctx = h.value                                        # for _seq
+        self._ctx = (h.value, self._index)                         # for _seq
 
     def close(self):
         if getattr(self, "h", None):
             self.lib.rh_destroy(self.h)
-            self.h, self._ctx = None, 0
+            self.h, self._ctx = None, (0, self._index)
 
     __del__ = close
 
