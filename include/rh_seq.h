@@ -60,7 +60,7 @@ typedef struct {
  *   new_off (dev out) i32 [n_streams + 1]: where each stream's slots begin; new_off[n_streams] = tokens granted.
  *   new_lengths (dev out) i32 [n_streams], new_count (dev out) i32 [1]: lengths and stack height afterwards; may be `lengths`
  *   and `free_count` themselves.  Of the table only the entries of granted pages are written.
- * Lengths below 0 count as 0, lengths past the table's row as the whole row when the stream ends.
+ * Lengths below 0 count as 0, lengths past the table's row as the whole row when the stream ends.  n_pages and the table's entries together stay below 2^31.
  */
 rh_status rh_cache_plan(rh_ctx* ctx, const int32_t* n_new, const int32_t* lengths, int32_t n_streams, int32_t page,
                         int32_t n_pages, int32_t max_pages, int32_t* block_table, int32_t* free_pages,

@@ -206,6 +206,9 @@ extern "C" rh_status rh_cache_plan(rh_ctx* ctx, const int32_t* n_new, const int3
         RH_FAIL(ctx, RH_E_SHAPE, "rh_cache_plan: page=%d, n_pages=%d, max_pages=%d, n_slots=%d must be positive (and n_slots below 2^31 - 16)", page, n_pages, max_pages, n_slots);
     if ((int64_t)page * n_pages > 0x7FFFFFFFll || (int64_t)page * max_pages > 0x7FFFFFFFll - page)
         RH_FAIL(ctx, RH_E_SHAPE, "rh_cache_plan: %d pages (%d a stream) of %d tokens pass 2^31 slots", n_pages, max_pages, page);
+    // whatever the lengths claim, ended streams give back no more pages than the table has entries: positions on the stack stay within 32 bits
+    if ((int64_t)n_streams * max_pages + n_pages > 0x7FFFFFFFll)
+        RH_FAIL(ctx, RH_E_SHAPE, "rh_cache_plan: %d rows of %d pages and a stack of %d pass 2^31 entries", n_streams, max_pages, n_pages);
     if (!n_new || !lengths || !block_table || !free_pages || !free_count || !slots || !new_off || !new_lengths || !new_count)
         RH_FAIL(ctx, RH_E_INVALID, "rh_cache_plan: null argument");
     plan_args a = {n_new, lengths, free_count, block_table, free_pages, slots, new_off, new_lengths, new_count, nullptr,
