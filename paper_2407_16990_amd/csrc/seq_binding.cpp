@@ -42,6 +42,12 @@ static int32_t word(PyObject* o, const char* why)           // what does not fit
     const long v = integer(o, why);
     return v > INT32_MAX ? INT32_MAX : v < INT32_MIN ? INT32_MIN : (int32_t)v;
 }
+static bool truth(PyObject* o, const char* why)
+{
+    const int v = PyObject_IsTrue(o);
+    need(v >= 0, why);                                       // what it raised stays
+    return v != 0;
+}
 static int32_t fits(int64_t v, const char* why) { need(v >= 0 && v <= INT32_MAX, why); return (int32_t)v; }
 // a call's context, and the tensors that it takes, which lie on its device
 struct context {
@@ -198,7 +204,7 @@ static PyObject* cache_attend(PyObject*, PyObject* const* a, Py_ssize_t nargs)
     const at::Tensor out = given(a[7]) ? on.tensor(a[7], "out on the GPU") : fresh(q.sizes(), q, q.scalar_type());
     need(out.scalar_type() == q.scalar_type() && out.is_contiguous() && out.sizes() == q.sizes(), "out as q, dense");
     at::Tensor lse;
-    if (PyObject_IsTrue(a[8])) lse = fresh({n, heads}, q, at::kFloat);
+    if (truth(a[8], "want_lse")) lse = fresh({n, heads}, q, at::kFloat);
     const int64_t qs[2] = {q.stride(0), q.stride(1)};
     const rh_status st = f_attend(on.handle, &c, q.data_ptr(), qs, type_of(q), heads, (const int32_t*)table.data_ptr(), fits(table.size(1), "block_table"),
                                   (const int32_t*)lengths.data_ptr(), n, (float)scale, window, out.data_ptr(), lse.defined() ? (float*)lse.data_ptr() : nullptr);
@@ -259,9 +265,9 @@ static PyObject* matvec_packed(PyObject*, PyObject* const* a, Py_ssize_t nargs)
     const at::ScalarType kind = given(a[6]) ? ((THPDtype*)a[6])->scalar_type : x.scalar_type() == at::kFloat ? at::kFloat : at::kBFloat16;
     const at::Tensor out = given(a[7]) ? on.tensor(a[7], "out on the GPU") : fresh({rows, n_out}, x, kind);
     need(out.dim() == 2 && out.size(0) == rows && out.size(1) == n_out && out.stride(1) == 1 && (!given(a[6]) || out.scalar_type() == kind), "out [rows, n_out]");
-    const int relu = PyObject_IsTrue(a[5]);
+    const bool relu = truth(a[5], "relu");
     const rh_status st = f_matvec(on.handle, x.data_ptr(), type_of(x), rows > 1 ? x.stride(0) : n_in, xs, (const uint8_t*)w.data_ptr(), (const uint8_t*)ws.data_ptr(),
-                                  rows, n_out, n_in, relu == 1, out.data_ptr(), type_of(out), rows > 1 ? out.stride(0) : n_out);
+                                  rows, n_out, n_in, relu, out.data_ptr(), type_of(out), rows > 1 ? out.stride(0) : n_out);
     if (st != RH_OK) return status(st);
     return wrap(out);
     END
