@@ -515,7 +515,9 @@ __global__ __launch_bounds__(ATTEND_T, D <= 128 ? 2 : 1) void k_seq_attend(atten
     uint64_t* rows = (uint64_t*)a.ws + ((size_t)first_row * units + unit) * ROW;
     uint32_t* counts = a.count + (size_t)first_row * units + unit;
     int at = split, members = n_split, stride = 1;           // the row that this workgroup has made, as the at-th of `members`, `stride` rows apart
-    // two levels of about as many each, where one does not do (121 chunks: 25.8 us with groups of 16, 24.9 with 12)
+    // two levels of about as many each, where one does not do.  Groups of 16 and of 12, us, one stream, 16 heads on 2 of 128 in bf16: 17 chunks 12.3 and 11.8, 48 12.4 and
+    // 11.9, 64 12.8 and 13.5, 96 14.7 and 14.4, 128 15.7 and 15.3; e4m3 12.1 and 11.6 (17), 13.8 and 13.5 (128); dim 256 18.7 and 17.6, 24.2 and 23.3; fp32 of 64 9.3
+    // and 9.3, 10.5 and 10.7
     const int fan = n_split > ATTEND_FAN && n_split <= 144 ? 12 : ATTEND_FAN;
     for (int level = 0; members > 1; ++level) {
         const int first = at / fan * fan, n = members - first < fan ? members - first : fan;
