@@ -70,8 +70,8 @@ rh_status rh_cache_plan(rh_ctx* ctx, const int32_t* n_new, const int32_t* length
 /*
  * Keys and values of n tokens into their slots.  k, v (dev): `type` (RH_T_F32 or RH_T_BF16), element (token, head, d) at
  * token*stride[0] + head*stride[1] + d.  slots (dev) i32 [n]; a slot outside [0, n_pages*page) is skipped (-1: a token that got no room).
- * Rounded to nearest even where the cache has fewer bits; RH_T_E4M3: scale = max(largest magnitude of the head, 2^-100) / 448,
- * element = value / scale rounded to e4m3, scale and quotient each rounded to fp32.  RH_E_UNIMPLEMENTED: bf16 values into an fp32 cache.
+ * Rounded to nearest even where the cache has fewer bits; RH_T_E4M3: scale = max(largest magnitude of the head, 2^-100) * (1/448),
+ * element = value / scale rounded to e4m3; 1/448, product and quotient are each rounded to fp32.  RH_E_UNIMPLEMENTED: bf16 values into an fp32 cache.
  * Slots of one call must differ.
  */
 rh_status rh_cache_write(rh_ctx* ctx, const rh_kv_cache* cache, const void* k, const int64_t k_stride[2], const void* v,
@@ -97,7 +97,7 @@ rh_status rh_cache_attend(rh_ctx* ctx, const rh_kv_cache* cache, const void* q, 
  *   s = x + residual (residual NULL: s = x),  y = s * weight / sqrt(mean(s^2) + eps)
  * with s unrounded.  Outputs, each may be NULL but not all:
  *   sum: s in `type` (may be `residual` or `x` itself);  y in `type`;
- *   y8, y8_scale (both or none): e4m3 [n_rows][n_cols] and f32 [n_rows], scale = max(largest |y| of the row, 2^-100) / 448, y8 = y / scale likewise.
+ *   y8, y8_scale (both or none): e4m3 [n_rows][n_cols] and f32 [n_rows], scale = max(largest |y| of the row, 2^-100) * (1/448), y8 = y / scale as there.
  * x, residual and sum have a row stride each (elements, >= n_cols); y and y8 are dense.  weight (dev) f32 [n_cols].
  */
 rh_status rh_norm_residual(rh_ctx* ctx, const void* x, int64_t x_stride, const void* residual, int64_t residual_stride,

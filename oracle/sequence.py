@@ -5,7 +5,7 @@ from __future__ import annotations
 import numpy as np
 
 AMAX_MIN = 2.0 ** -100
-E4M3_MAX = 448.0
+E4M3_MAX = 448.0                      # scales are amax / 448; the kernels' product with 1/448 is within an ulp of fp32
 FP4 = np.array([0, 0.5, 1, 1.5, 2, 3, 4, 6, -0.0, -0.5, -1, -1.5, -2, -3, -4, -6])
 
 

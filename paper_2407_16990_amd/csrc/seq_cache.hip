@@ -219,7 +219,7 @@ extern "C" rh_status rh_cache_plan(rh_ctx* ctx, const int32_t* n_new, const int3
 // ---------------------------------------------------------------------------------------------------------------
 // rh_cache_write
 // ---------------------------------------------------------------------------------------------------------------
-// Bound by memory: every key and value read and written once (27600 tokens of 8 heads of 128, bf16 to e4m3: 171 MB in 40 to 46 us, 3.7 to 4.3 TB/s; half the
+// Bound by memory: every key and value read and written once (27600 tokens of 8 heads of 128, bf16 to e4m3: 171 MB in 39 to 45 us, 3.8 to 4.4 TB/s; half the
 // bytes written go to scattered slots, a quarter of a KB at a time).  G lanes (a power of two) take a head's row, eight elements each, so
 // that the largest magnitude is a few lane exchanges; lanes past the head's size idle.
 // Rows a thread, whose loads are in flight together: two where they are quantised (27600 tokens of 8 heads of 128, with quotients not yet corrected: 44.1 us, one row

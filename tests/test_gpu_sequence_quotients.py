@@ -1,5 +1,5 @@
-"""8-bit outputs of the sequence operators bit for bit: scale = max(largest magnitude, 2^-100) / 448 and element = value / scale, each rounded
-once to fp32, the element then to e4m3 (nearest, ties to even).  No tolerance: the same steps in numpy and torch on the CPU give the same codes."""
+"""8-bit outputs of the sequence operators bit for bit: scale = max(largest magnitude, 2^-100) * (1/448) and element = value / scale, 1/448, product and quotient
+each rounded to fp32, the element then to e4m3 (nearest, ties to even).  No tolerance: the same steps in numpy and torch on the CPU give the same codes."""
 import numpy as np
 import pytest
 import torch
@@ -12,7 +12,7 @@ pytestmark = pytest.mark.gpu
 def _codes(v):
     """v f32 [rows, n] -> (codes uint8 [rows, n], scales f32 [rows])."""
     v = v.astype(np.float32)
-    scale = np.maximum(np.abs(v).max(-1), np.float32(2.0 ** -100)) / np.float32(448)
+    scale = np.maximum(np.abs(v).max(-1), np.float32(2.0 ** -100)) * (np.float32(1) / np.float32(448))
     assert scale.dtype == np.float32
     return torch.from_numpy(v / scale[:, None]).to(E4M3).view(torch.uint8).numpy(), scale
 
@@ -60,3 +60,19 @@ def test_norm_gives_the_codes_of_the_quotients(rh, dtype, rows, cols):  # noqa: 
         assert np.array_equal(sc.cpu().numpy(), scales)
         got = y8.view(torch.uint8).cpu().numpy()
         assert np.array_equal(got, codes), (most, int((got != codes).sum()))
+
+
+def test_write_and_norm_are_torchs_formula_on_the_gpu(rh):  # noqa: F811
+    """The formula in torch's operations on the same device gives the same bits: t / 448.0 is a product with 1/448 there."""
+    g = torch.Generator(device="cuda").manual_seed(0)
+    x = torch.randn((500, 4, 96), generator=g, device="cuda").to(torch.bfloat16)
+    cache = _empty_cache(40, 16, 4, 96, E4M3, "token")
+    rh.cache_write(cache, x, x, torch.arange(500, dtype=torch.int32, device="cuda"))
+    scale = x.float().abs().amax(-1).clamp_min(2.0 ** -100) / 448.0
+    codes = (x.float() / scale[..., None]).to(E4M3).view(torch.uint8)
+    got = cache.k.view(torch.uint8).reshape(-1, 4, 96)[:500], cache.k_scale.transpose(1, 2).reshape(-1, 4)[:500]
+    assert torch.equal(got[0], codes) and torch.equal(got[1], scale)
+    y = torch.randn((300, 700), generator=g, device="cuda")
+    _, n, n8, sc = rh.norm_residual(y, torch.ones(700, device="cuda"), outputs="both")
+    scale = n.abs().amax(-1).clamp_min(2.0 ** -100) / 448.0
+    assert torch.equal(sc, scale) and torch.equal(n8.view(torch.uint8), (n / scale[:, None]).to(E4M3).view(torch.uint8))
