@@ -2,7 +2,7 @@
 //
 // Bound by memory: every key and value of a stream is read once for all query heads that share it.  The scores and the sums go on the
 // matrix cores, which have rate to spare even where a tile of 16 heads is mostly empty (64 streams of up to 8192 tokens, bf16, 32 heads
-// on 8 of 128: 202 us, 5.2 TB/s, as much as a copy has; they work 5 % of the time), so that one kernel serves every number of heads a key,
+// on 8 of 128: 204 us, 5.2 TB/s, as much as a copy has; they work 7 % of the time), so that one kernel serves every number of heads a key,
 // and vector instructions are left for the softmax.
 //
 // A wave takes a tile of tokens (32; 16 of an fp32 cache) at a time, with no barrier in its loop:
@@ -20,8 +20,8 @@
 // among short ones keeps every CU busy.  How long a chunk is follows from the lengths, which the host does not know: every
 // wave (of more than 64 streams, every workgroup) adds them up and finds its own chunk.  The chunks of a stream and unit leave their
 // sums, maxima and totals in scratch memory; of every 16 the one that finishes last joins them, in their order, and so on up.  One stream
-// of 108000 tokens (e4m3, 16 heads on 2 of 128: 242 chunks, two levels): 24.2 us, where its bytes take 10.9; 5 are a call's on one tile, and
-// about 3 each level.
+// of 108000 tokens (e4m3, 16 heads on 2 of 128: 242 chunks, two levels): 24.7 us, where its bytes take 10.9; 5 are a call's on one tile,
+// about 3 each level, and the four waves a CU that this gives keep too few bytes in flight.
 #include "seq_common.h"
 
 struct attend_args {
