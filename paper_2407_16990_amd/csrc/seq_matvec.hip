@@ -494,7 +494,7 @@ static hipError_t launch_matvec(rh_ctx* ctx, matvec_args a)
     };
     // The inner index may be cut into slices too, a workgroup each, whose sums are joined in the same launch: where x is long, or the tiles are
     // few, a workgroup's slice of x takes less than the whole of it.  A line through times of 72 shapes (1 to 64 rows, 64 to 4096 outputs, 1024 to
-    // 16384 inputs, every type of row) at nine numbers of slices, 10 % off in the mean, tells when: 25 us a MB of x laid out in LDS, 14 a MB of weights
+    // 16384 inputs, fp32 and bf16 rows and 8-bit ones on a product since taken out) at nine numbers of slices, 10 % off in the mean, tells when: 25 us a MB of x laid out in LDS, 14 a MB of weights
     // that a workgroup reads, 1.7 a stretch that a wave goes through one after another, 2.9 for the join, 1 more for a second batch of loads there, 1.1 a MB
     // of sums.  What it picks is 1 % slower than the best of the nine in the mean, 11 % at most.  fp32 rows, 16 x 256 x 16384: 64.6 us as a
     // whole, 12.9 in 16 slices; 1 x 4096 x 1024 5.6 and 8.3 in two.
