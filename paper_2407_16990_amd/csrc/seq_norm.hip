@@ -5,7 +5,7 @@
 // A row belongs to one wave where it is short, so that a workgroup of four waves needs no barrier, or to a part of one where it is shorter still.
 // 14720 x 4095 of fp32, all outputs: 183 us, 5.6 TB/s; of bf16 126, 4.3 TB/s (rows at odd addresses; 4092: 108, 5.0 TB/s); 8 x 1024 of
 // bf16, 8-bit output, 3.7, hardly more than an empty launch and a way to memory.
-#include "seq_common.h"
+#include "seq_rows.h"
 
 struct norm_args {
     const void *x, *residual;
@@ -17,61 +17,6 @@ struct norm_args {
     int32_t rows, cols;
     float eps;
 };
-
-// 16 bytes of a row of `cols` elements from element c on, of which the row may have fewer: all lanes load whole pieces that lie in the
-// row, the last ones from further ahead, and norm_place moves those to their place, with zeros behind.  (A branch for them, element by
-// element, was a way to memory of its own: 14720 x 4092 of bf16 126 us, now 108.)
-template <typename T, int E>
-__device__ __forceinline__ u32x4 norm_load(const T* row, int c, int cols)
-{
-    if (cols >= E) return seq_load<u32x4>(row + (c < cols - E ? c : cols - E));
-    u32x4 w = {0, 0, 0, 0};                                  // a row shorter than a piece
-#pragma unroll
-    for (int i = 0; i < E; ++i)
-        if (c + i < cols) w[i * (int)sizeof(T) / 4] |= sizeof(T) == 4 ? *(const uint32_t*)(row + c + i) : (uint32_t)*(const uint16_t*)(row + c + i) << (16 * (i & 1));
-    return w;
-}
-template <typename T, int E>
-__device__ __forceinline__ void norm_place(u32x4 w, int c, int cols, float (&v)[E])
-{
-    const int s = cols >= E && c > cols - E ? c - (cols - E) : 0;            // elements that w is ahead by
-    if (__any(s)) {
-        constexpr int W = 4 / sizeof(T);                     // elements of a word
-        if (s & 2 * W) w = u32x4{w[2], w[3], 0, 0};
-        if (s & W) w = u32x4{w[1], w[2], w[3], 0};
-        if (W == 2 && (s & 1))
-            w = u32x4{w[0] >> 16 | w[1] << 16, w[1] >> 16 | w[2] << 16, w[2] >> 16 | w[3] << 16, w[3] >> 16};
-        if (s >= E) w = u32x4{0, 0, 0, 0};
-    }
-    if constexpr (sizeof(T) == 2) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { v[2 * i] = seq_bf16_lo(w[i]); v[2 * i + 1] = seq_bf16_hi(w[i]); }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(w[i]);
-    }
-}
-
-// the first `bytes` of w, or all 16; whole elements of B bytes
-template <int B>
-__device__ __forceinline__ void norm_put(uint8_t* p, int bytes, u32x4 w)
-{
-    if (bytes >= 16) { seq_store(p, w); return; }
-    if (bytes & 8) { seq_store(p, make_uint2(w[0], w[1])); p += 8; w = u32x4{w[2], w[3], 0, 0}; }
-    if (bytes & 4) { seq_store(p, w[0]); p += 4; w[0] = w[1]; }
-    if (B < 4 && (bytes & 2)) { seq_store(p, (uint16_t)w[0]); p += 2; w[0] >>= 16; }
-    if (B < 2 && (bytes & 1)) *p = (uint8_t)w[0];
-}
-
-template <typename T, int E>
-__device__ __forceinline__ void norm_store(T* p, int n, const float (&v)[E])
-{
-    u32x4 w;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-        if constexpr (sizeof(T) == 2) w[i] = seq_pack_bf16(v[2 * i], v[2 * i + 1]); else w[i] = __float_as_uint(v[i]);
-    norm_put<(int)sizeof(T)>((uint8_t*)p, n * (int)sizeof(T), w);
-}
 
 // The sum (MAX: the largest, a NaN staying) of a value of every thread of a row's WAVES waves, or of its LANES lanes.
 template <int WAVES, int LANES, bool MAX>
@@ -105,18 +50,18 @@ __global__ __launch_bounds__(WAVES > 1 ? WAVES * 64 : 256) void k_seq_norm(norm_
     float v[ITEMS][E], square = 0.f;
     u32x4 in[ITEMS], add[ITEMS];
 #pragma unroll
-    for (int i = 0; i < ITEMS; ++i) in[i] = norm_load<T, E>(x, (t + i * NT) * E, a.cols);
+    for (int i = 0; i < ITEMS; ++i) in[i] = row_load<T, E>(x, (t + i * NT) * E, a.cols);
     if (a.residual) {
 #pragma unroll
-        for (int i = 0; i < ITEMS; ++i) add[i] = norm_load<T, E>(r, (t + i * NT) * E, a.cols);
+        for (int i = 0; i < ITEMS; ++i) add[i] = row_load<T, E>(r, (t + i * NT) * E, a.cols);
     }
 #pragma unroll
-    for (int i = 0; i < ITEMS; ++i) norm_place<T, E>(in[i], (t + i * NT) * E, a.cols, v[i]);
+    for (int i = 0; i < ITEMS; ++i) row_place<T, E>(in[i], (t + i * NT) * E, a.cols, v[i]);
     if (a.residual) {
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {
             float u[E];
-            norm_place<T, E>(add[i], (t + i * NT) * E, a.cols, u);
+            row_place<T, E>(add[i], (t + i * NT) * E, a.cols, u);
 #pragma unroll
             for (int e = 0; e < E; ++e) v[i][e] += u[e];
         }
@@ -131,7 +76,7 @@ __global__ __launch_bounds__(WAVES > 1 ? WAVES * 64 : 256) void k_seq_norm(norm_
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {
             const int c = (t + i * NT) * E, n = a.cols - c;
-            if (n > 0) norm_store<T, E>(s + c, n, v[i]);
+            if (n > 0) row_store<T, E>(s + c, n, v[i]);
         }
     }
     if (!a.y && !a.y8) return;
@@ -144,7 +89,7 @@ __global__ __launch_bounds__(WAVES > 1 ? WAVES * 64 : 256) void k_seq_norm(norm_
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i)
 #pragma unroll
-            for (int e = 0; e < E; e += 4) weight[i][e / 4] = norm_load<float, 4>(a.weight, (t + (i0 + i) * NT) * E + e, a.cols);
+            for (int e = 0; e < E; e += 4) weight[i][e / 4] = row_load<float, 4>(a.weight, (t + (i0 + i) * NT) * E + e, a.cols);
 #pragma unroll
         for (int i = i0; i < i0 + AHEAD; ++i) {
             const int c = (t + i * NT) * E, n = a.cols - c;
@@ -152,7 +97,7 @@ __global__ __launch_bounds__(WAVES > 1 ? WAVES * 64 : 256) void k_seq_norm(norm_
 #pragma unroll
             for (int e = 0; e < E; e += 4) {
                 float u[4];
-                norm_place<float, 4>(weight[i - i0][e / 4], c + e, a.cols, u);
+                row_place<float, 4>(weight[i - i0][e / 4], c + e, a.cols, u);
 #pragma unroll
                 for (int k = 0; k < 4; ++k) w[e + k] = u[k];
             }
@@ -162,7 +107,7 @@ __global__ __launch_bounds__(WAVES > 1 ? WAVES * 64 : 256) void k_seq_norm(norm_
                 const float m = fabsf(v[i][e]);
                 most = m != m || m > most ? m : most;
             }
-            if (a.y && n > 0) norm_store<T, E>((T*)a.y + (int64_t)row * a.cols + c, n, v[i]);
+            if (a.y && n > 0) row_store<T, E>((T*)a.y + (int64_t)row * a.cols + c, n, v[i]);
         }
     }
     if (!a.y8) return;
@@ -178,7 +123,7 @@ __global__ __launch_bounds__(WAVES > 1 ? WAVES * 64 : 256) void k_seq_norm(norm_
         u32x4 q = {0, 0, 0, 0};
 #pragma unroll
         for (int e = 0; e < E; e += 4) q[e / 4] = seq_pack_scaled(v[i][e], v[i][e + 1], v[i][e + 2], v[i][e + 3], y8_scale);
-        if (n < E) norm_put<1>(o, n, q);
+        if (n < E) row_put<1>(o, n, q);
         else if constexpr (E == 8) seq_store(o, make_uint2(q[0], q[1]));
         else seq_store(o, q[0]);
     }
