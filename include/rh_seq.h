@@ -1,5 +1,5 @@
 /*
- * rh_seq.h - operators of a transformer's decode step over many live streams (gfx950).
+ * rh_seq.h - operators of a transformer's or a state-space model's step over many live streams (gfx950).
  *
  * What precedes rh_select_regions on live streams is a score for every macroblock of each frame as it arrives.  A
  * predictor that remembers a stream's past runs one token per stream and frame: these are the operators of such a step.
@@ -8,11 +8,15 @@
  *   rh_cache_attend    attention of one new token of every stream over the stream's cached tokens
  *   rh_norm_residual   residual addition and root-mean-square norm, output also in 8 bits with a scale a row
  *   rh_matvec_packed   products of a few rows with weights in 4 bits that share a scale by 32
+ * and those of a layer that keeps a state of fixed size for a stream instead of a cache, for one token of every stream or for many:
+ *   rh_state_conv      short causal convolution along a stream's tokens, its last inputs kept
+ *   rh_state_scan      selective scan of a stream's state over its tokens
+ *   rh_norm_gated      root-mean-square norm of gated rows over groups of channels, output also in 8 bits
  * They take a context of rh.h and follow its conventions: device pointers, caller-owned buffers, all work on the context's
  * stream, arguments checked before any launch, rh_last_error.  They use neither the context's network nor its capacities,
  * and count in no class of rh_profile_read.  Sums, softmax statistics and norms are held in 32 bits.
- * Scratch memory of rh_cache_attend and rh_matvec_packed (68 MB on 256 CUs) and a few counters, of rh_cache_plan too, belong to the context: the first call that wants
- * them allocates them and waits for the stream, and no later one does.  Graphs may be recorded once an rh_cache_attend or rh_matvec_packed call of the context has been made
+ * Scratch memory of rh_cache_attend, rh_matvec_packed and rh_state_scan (68 MB on 256 CUs) and a few counters, of rh_cache_plan too, belong to the context: the first call that wants
+ * them allocates them and waits for the stream, and no later one does.  Graphs may be recorded once an rh_cache_attend or rh_matvec_packed call, or an rh_state_scan call of more than one token a stream, of the context has been made
  * (RH_E_STATE where a captured call would have to allocate).  Since calls share this memory, those of one context must not overlap on two streams, replays of
  * a graph that recorded them among them: use a context for each, or let one wait for the other.
  */
@@ -117,6 +121,65 @@ rh_status rh_norm_residual(rh_ctx* ctx, const void* x, int64_t x_stride, const v
 rh_status rh_matvec_packed(rh_ctx* ctx, const void* x, int32_t x_type, int64_t x_stride, const float* x_scale,
                            const uint8_t* w, const uint8_t* w_scale, int32_t n_rows, int32_t n_out, int32_t n_in,
                            int32_t relu, void* y, int32_t y_type, int64_t y_stride);
+
+#define RH_SEQ_MAX_TAPS 8                              /* width of rh_state_conv                      */
+#define RH_SEQ_MAX_CHANNELS 65536                      /* of rh_state_scan                           */
+#define RH_SEQ_MAX_STATE 128                           /* elements of a channel's state in rh_state_scan */
+#define RH_SEQ_MAX_GROUPS 1024                         /* of a row in rh_norm_gated                   */
+
+/*
+ * The rows (tokens) of a call and where their streams' states lie in a pool of n_slots, all in device memory.
+ *   offsets i32 [n_streams + 1], ascending: rows [offsets[b], offsets[b+1]) are the new tokens of stream b, in order; rows of no stream are left as they are.
+ *     NULL: one row a stream (n_rows = n_streams).  Offsets outside [0, n_rows] count as its ends.
+ *   slots i32 [n_streams]: the stream's state before the call; into i32 [n_streams] (NULL: slots): where its state afterwards goes, so
+ *     that the one before may stay.  A slot outside [0, n_slots): a state of zeros; an `into` outside: not kept.
+ *   past i32 [n_streams] (NULL: all have one): 0 or below where a stream begins with this call: its state before is zeros, whatever its slot holds.
+ * A stream without rows has nothing of its states read or written.  Streams may share a slot that they read; what one writes no other reads or writes.
+ */
+typedef struct {
+    const int32_t *offsets, *slots, *into, *past;
+    int32_t n_streams, n_rows, n_slots;                /* n_streams at most RH_SEQ_MAX_STREAMS where there are offsets */
+} rh_state_rows;
+
+/*
+ * Depthwise causal convolution along the tokens of every stream: y[t][c] = act(bias[c] + sum_j weight[j][c] * x[t - (width-1) + j][c]),
+ * act(v) = v / (1 + exp(-v)) where silu is not 0; ahead of the stream's first row of the call x is the state.
+ *   x, y (dev): `type` (RH_T_F32 or RH_T_BF16), rows x_stride and y_stride elements apart (>= channels); they must not overlap.
+ *   weight (dev) f32 [width][channels], 2 <= width <= RH_SEQ_MAX_TAPS; bias (dev) f32 [channels] or NULL.
+ *   state (dev, in/out): `type`, [n_slots][width-1][channels]: the last inputs, the latest last.
+ */
+rh_status rh_state_conv(rh_ctx* ctx, const rh_state_rows* rows, const void* x, int64_t x_stride, const float* weight,
+                        const float* bias, int32_t type, int32_t channels, int32_t width, int32_t silu, void* state,
+                        void* y, int64_t y_stride);
+
+/*
+ * Selective scan along the tokens of every stream, for every channel c with its n states, and group g of channels (channels / groups neighbours):
+ *   delta = dt[t][c] + dt_bias[c], with softplus not 0 log(1 + exp(that));   h[c][i] = exp(delta * a[c][i]) * h[c][i] + delta * x[t][c] * b[t][g][i]
+ *   y[t][c] = sum_i c[t][g][i] * h[c][i] + skip[c] * x[t][c], with a gate times gate[t][c] / (1 + exp(-gate[t][c]))
+ *   x, dt, gate (NULL: none) and y (dev): `type` (RH_T_F32 or RH_T_BF16), rows x_stride ... y_stride elements apart (>= channels); y overlaps none of the inputs.
+ *   b, c (dev): `type`, element (t, g, i) at t*b_stride + g*n + i (b_stride, c_stride >= groups*n).
+ *   a (dev) f32 [channels][n]; dt_bias, skip (dev) f32 [channels], each may be NULL; channels <= RH_SEQ_MAX_CHANNELS, 1 <= n <= RH_SEQ_MAX_STATE; groups divides channels.
+ *   state (dev, in/out) f32 [n_slots][channels][n].
+ * Streams that are long for the call are cut into chunks, which are scanned side by side: from zeros first, for what each adds to the state
+ * behind it, and again from the state that the chunks ahead leave.  Sums come in the same order every time.
+ */
+typedef struct {
+    const void *x, *dt, *gate, *b, *c;
+    int64_t x_stride, dt_stride, gate_stride, b_stride, c_stride;
+    const float *a, *dt_bias, *skip;
+    int32_t type, channels, groups, n, softplus;
+} rh_scan_inputs;
+rh_status rh_state_scan(rh_ctx* ctx, const rh_state_rows* rows, const rh_scan_inputs* in, float* state, void* y, int64_t y_stride);
+
+/*
+ * Gate and root-mean-square norm of n_rows rows of n_cols <= RH_SEQ_MAX_COLS elements of `type` (RH_T_F32 or RH_T_BF16), in `groups` groups of neighbours:
+ *   s = x * gate / (1 + exp(-gate)),  y = s * weight / sqrt(mean over its group(s^2) + eps)
+ * Outputs y (in `type`) and y8 with y8_scale as in rh_norm_residual, dense; each may be NULL but not all.  x and gate have a row stride each
+ * (elements, >= n_cols).  weight (dev) f32 [n_cols]; groups <= RH_SEQ_MAX_GROUPS divides n_cols.
+ */
+rh_status rh_norm_gated(rh_ctx* ctx, const void* x, int64_t x_stride, const void* gate, int64_t gate_stride, const float* weight,
+                        int32_t type, int32_t n_rows, int32_t n_cols, int32_t groups, float eps, void* y, uint8_t* y8,
+                        float* y8_scale);
 
 #ifdef __cplusplus
 }

@@ -72,7 +72,8 @@ class _Sequence:
         spec = importlib.util.spec_from_file_location("_seq", _b.MODULE)
         module = importlib.util.module_from_spec(spec)
         spec.loader.exec_module(module)
-        module.init(*[C.cast(f, C.c_void_p).value for f in (L.rh_cache_plan, L.rh_cache_write, L.rh_cache_attend, L.rh_norm_residual, L.rh_matvec_packed)])
+        module.init(*[C.cast(f, C.c_void_p).value for f in (L.rh_cache_plan, L.rh_cache_write, L.rh_cache_attend, L.rh_norm_residual, L.rh_matvec_packed,
+                                                                    L.rh_state_conv, L.rh_state_scan, L.rh_norm_gated)])
         self.__dict__.update({n: f for n, f in vars(module).items() if not n.startswith("__")})        # from here on without this function
         return self.__dict__[name]
 
@@ -131,6 +132,9 @@ def load_library():
     L.rh_cache_attend.argtypes = [vp, vp, vp, vp, i32, i32, vp, i32, vp, i32, f32, i32, vp, vp]
     L.rh_norm_residual.argtypes = [vp, vp, i64, vp, i64, vp, i32, i32, i32, f32, vp, i64, vp, vp, vp]
     L.rh_matvec_packed.argtypes = [vp, vp, i32, i64, vp, vp, vp, i32, i32, i32, i32, vp, i32, i64]
+    L.rh_state_conv.argtypes = [vp, vp, vp, i64, vp, vp, i32, i32, i32, i32, vp, vp, i64]
+    L.rh_state_scan.argtypes = [vp, vp, vp, vp, vp, i64]
+    L.rh_norm_gated.argtypes = [vp, vp, i64, vp, i64, vp, i32, i32, i32, i32, f32, vp, vp, vp]
     L.rh_select_regions_noalloc.argtypes = [vp, i32, i32, i32, C.POINTER(Segment), i32, i32, vp, vp, vp, vp]
     _lib = L
     return L
@@ -404,7 +408,7 @@ class RH:
         self._check(self.lib.rh_temporal_spread(self.h, _ptr(importance), importance.shape[0], _ptr(selected), _ptr(reuse_from)))
         return importance
 
-    # -- operators of a decode step over many streams (include/rh_seq.h) -------------------------
+    # -- operators of a step over many streams (include/rh_seq.h) -------------------------
     def _outputs(self, got):
         """What a call of _seq returned: a status (0 aside) raises.  Outputs, made on torch's current stream, are held back from
         reuse until the library's stream, should it be another, is past them."""
@@ -447,6 +451,29 @@ class RH:
         """x [rows, n_in] (float32, bfloat16, or float8_e4m3fn with x_scale f32 [rows]) by weights in 4 bits: w uint8
         [n_out, 16 * ceil(n_in / 32)], w_scale uint8 [n_out, ceil(n_in / 32)] (pack_weights makes them) -> [rows, n_out]."""
         return self._outputs(_seq.matvec_packed(self._ctx, x, w, w_scale, x_scale, relu, out_dtype, out))
+
+    def state_conv(self, x: torch.Tensor, weight: torch.Tensor, state: torch.Tensor, slots: torch.Tensor, bias: torch.Tensor | None = None,
+                   offsets: torch.Tensor | None = None, past: torch.Tensor | None = None, into: torch.Tensor | None = None, silu: bool = True,
+                   out: torch.Tensor | None = None) -> torch.Tensor:
+        """Causal convolution of every channel along each stream's rows, weight f32 [width, channels] and bias f32 [channels], then SiLU -> as x
+        [rows, channels] (float32 or bfloat16, last stride 1).  A row a stream, or rows offsets[b] to offsets[b + 1] (int32 [n_streams + 1], ascending)
+        of stream b; what no stream has of `out` stays.  state [n_slots, width - 1, channels] of x's type holds every stream's last inputs,
+        replaced in place: read from slots int32 [n_streams] (zeros for -1, and where past, int32 [n_streams], is 0), written to `into` (None: slots; -1: not kept)."""
+        return self._outputs(_seq.state_conv(self._ctx, x, weight, state, slots, bias, offsets, past, into, silu, out))
+
+    def state_scan(self, x: torch.Tensor, dt: torch.Tensor, a: torch.Tensor, b: torch.Tensor, c: torch.Tensor, state: torch.Tensor, slots: torch.Tensor,
+                   skip: torch.Tensor | None = None, gate: torch.Tensor | None = None, dt_bias: torch.Tensor | None = None, softplus: bool = True,
+                   offsets: torch.Tensor | None = None, past: torch.Tensor | None = None, into: torch.Tensor | None = None,
+                   out: torch.Tensor | None = None) -> torch.Tensor:
+        """Selective scan along each stream's rows: delta = softplus(dt + dt_bias), h = exp(delta a) h + delta x b, y = c.h + skip x, times SiLU(gate)
+        -> as x [rows, channels].  dt and gate are as x, b and c [rows, groups, n] of its type, a f32 [channels, n], skip and dt_bias f32
+        [channels]; h is in state f32 [n_slots, channels, n].  Rows, slots, past and into as in state_conv."""
+        return self._outputs(_seq.state_scan(self._ctx, x, dt, a, b, c, state, slots, skip, gate, dt_bias, softplus, offsets, past, into, out))
+
+    def norm_gated(self, x: torch.Tensor, gate: torch.Tensor, weight: torch.Tensor, groups: int = 1, eps: float = 1e-6, outputs: str = "same"):
+        """x * SiLU(gate) [rows, cols], each of `groups` groups of neighbouring columns normed by its root mean square, weighted -> (y, y8, y8_scale), None
+        where not asked for: y for outputs "same" or "both", y8 float8_e4m3fn with y8_scale f32 [rows] for "e4m3" or "both"."""
+        return self._outputs(_seq.norm_gated(self._ctx, x, gate, weight, groups, eps, outputs))
 
     def read_counts(self, counts: torch.Tensor):
         out = (C.c_uint32 * 4)()

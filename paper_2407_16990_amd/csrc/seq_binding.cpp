@@ -17,6 +17,9 @@ static decltype(&rh_cache_write) f_write;
 static decltype(&rh_cache_attend) f_attend;
 static decltype(&rh_norm_residual) f_norm;
 static decltype(&rh_matvec_packed) f_matvec;
+static decltype(&rh_state_conv) f_conv;
+static decltype(&rh_state_scan) f_scan;
+static decltype(&rh_norm_gated) f_gated;
 
 struct refused { const char* why; };
 static void need(bool ok, const char* why) { if (!ok) throw refused{why}; }
@@ -213,6 +216,18 @@ static PyObject* cache_attend(PyObject*, PyObject* const* a, Py_ssize_t nargs)
     END
 }
 
+// which outputs of a norm are asked for
+struct kinds {
+    bool plain, quantised;
+    explicit kinds(PyObject* o)
+    {
+        auto is = [&](const char* name) { return PyUnicode_Check(o) && !PyUnicode_CompareWithASCIIString(o, name); };
+        const bool both = is("both");
+        plain = is("same") || both; quantised = is("e4m3") || both;
+        need(plain || quantised, "outputs \"same\", \"e4m3\" or \"both\"");
+    }
+};
+
 // norm_residual(ctx, x, weight, residual, eps, outputs, sum_out) -> (sum, y, y8, y8_scale), None where not asked for
 static PyObject* norm_residual(PyObject*, PyObject* const* a, Py_ssize_t nargs)
 {
@@ -224,8 +239,7 @@ static PyObject* norm_residual(PyObject*, PyObject* const* a, Py_ssize_t nargs)
     const int32_t rows = fits(x.size(0), "x"), cols = fits(x.size(1), "x");
     const double eps = PyFloat_AsDouble(a[4]);
     need(!PyErr_Occurred(), "eps");
-    const bool same = PyUnicode_Check(a[5]) && !PyUnicode_CompareWithASCIIString(a[5], "same"), both = PyUnicode_Check(a[5]) && !PyUnicode_CompareWithASCIIString(a[5], "both");
-    need(same || both || (PyUnicode_Check(a[5]) && !PyUnicode_CompareWithASCIIString(a[5], "e4m3")), "outputs \"same\", \"e4m3\" or \"both\"");
+    const kinds out(a[5]);
     at::Tensor residual, sum, y, y8, scale;
     if (given(a[3])) {
         residual = on.tensor(a[3], "residual on the GPU");
@@ -233,8 +247,8 @@ static PyObject* norm_residual(PyObject*, PyObject* const* a, Py_ssize_t nargs)
         sum = given(a[6]) ? on.tensor(a[6], "sum_out on the GPU") : fresh(x.sizes(), x, x.scalar_type());
         need(sum.scalar_type() == x.scalar_type() && sum.sizes() == x.sizes() && sum.stride(1) == 1, "sum_out as x");
     }
-    if (same || both) y = fresh(x.sizes(), x, x.scalar_type());
-    if (!same) { y8 = fresh(x.sizes(), x, at::kFloat8_e4m3fn); scale = fresh({rows}, x, at::kFloat); }
+    if (out.plain) y = fresh(x.sizes(), x, x.scalar_type());
+    if (out.quantised) { y8 = fresh(x.sizes(), x, at::kFloat8_e4m3fn); scale = fresh({rows}, x, at::kFloat); }
     auto row = [&](const at::Tensor& t) { return t.defined() && rows > 1 ? t.stride(0) : (int64_t)cols; };
     auto at_ = [](const at::Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; };
     const rh_status st = f_norm(on.handle, x.data_ptr(), row(x), at_(residual), row(residual), (const float*)weight.data_ptr(), type_of(x), rows, cols,
@@ -273,20 +287,157 @@ static PyObject* matvec_packed(PyObject*, PyObject* const* a, Py_ssize_t nargs)
     END
 }
 
-// init(plan, write, attend, norm, matvec): addresses of the library's functions
+// The rows and states of a call: offsets, slots, past and into, the state's first dimension being the pool.
+static rh_state_rows rows_of(const context& on, PyObject* offsets, PyObject* slots, PyObject* past, PyObject* into, int64_t n_rows, int64_t n_slots)
+{
+    rh_state_rows r = {};
+    const at::Tensor& s = on.dense(slots, at::kInt, "slots int32, dense");
+    r.slots = (const int32_t*)s.data_ptr();
+    r.n_streams = fits(s.numel(), "slots"); r.n_rows = fits(n_rows, "rows"); r.n_slots = fits(n_slots, "state");
+    if (given(offsets)) {
+        const at::Tensor& t = on.dense(offsets, at::kInt, "offsets int32, dense");
+        need(t.numel() == s.numel() + 1, "offsets [n_streams + 1]");
+        r.offsets = (const int32_t*)t.data_ptr();
+    } else need(n_rows == s.numel(), "a row for every stream, or offsets");
+    for (int i = 0; i < 2; ++i) {
+        PyObject* o = i ? into : past;
+        if (!given(o)) continue;
+        const at::Tensor& t = on.dense(o, at::kInt, i ? "into int32, dense" : "past int32, dense");
+        need(t.numel() == s.numel(), "past and into as long as slots");
+        (i ? r.into : r.past) = (const int32_t*)t.data_ptr();
+    }
+    return r;
+}
+// a matrix whose rows' elements lie side by side, of `like`'s type and shape
+static const at::Tensor& as(const context& on, PyObject* o, const at::Tensor& like, const char* why)
+{
+    const at::Tensor& t = on.tensor(o, why);
+    need(t.scalar_type() == like.scalar_type() && t.sizes() == like.sizes() && t.stride(1) == 1, why);
+    return t;
+}
+static int64_t row_stride(const at::Tensor& t) { return t.size(0) > 1 ? t.stride(0) : t.size(1); }
+// no element of one matrix lies in the other: all of it ahead or behind, or columns side by side in rows of one length
+static bool apart(const at::Tensor& a, const at::Tensor& b)
+{
+    if (!a.numel() || !b.numel()) return true;
+    const int64_t size = (int64_t)a.element_size(), wide = row_stride(a) * size, p = (int64_t)a.data_ptr(), q = (int64_t)b.data_ptr();
+    auto bytes = [&](const at::Tensor& t) { return ((t.size(0) - 1) * row_stride(t) + t.size(1)) * size; };
+    if (p + bytes(a) <= q || q + bytes(b) <= p) return true;
+    if (row_stride(a) != row_stride(b) || a.size(0) < 2) return false;
+    const int64_t at = ((q - p) % wide + wide) % wide;       // b's columns in a's rows
+    return at >= a.size(1) * size && at + b.size(1) * size <= wide;
+}
+
+// state_conv(ctx, x, weight, state, slots, bias, offsets, past, into, silu, out) -> out
+static PyObject* state_conv(PyObject*, PyObject* const* a, Py_ssize_t nargs)
+{
+    BEGIN
+    need(nargs == 11, "eleven arguments");
+    const context on(a[0]);
+    const at::Tensor &x = on.tensor(a[1], "x on the GPU"), &weight = on.dense(a[2], at::kFloat, "weight float32, dense"), &state = on.tensor(a[3], "state on the GPU");
+    need(x.dim() == 2 && x.stride(1) == 1, "x [rows, channels], elements side by side");
+    need(weight.dim() == 2 && weight.size(1) == x.size(1), "weight [width, channels]");
+    const int32_t channels = fits(x.size(1), "channels"), width = fits(weight.size(0), "width");
+    need(state.scalar_type() == x.scalar_type() && state.is_contiguous() && state.dim() == 3 && state.size(1) == width - 1 && state.size(2) == channels,
+         "state as x, dense, [n_slots, width - 1, channels]");
+    const float* bias = nullptr;
+    if (given(a[5])) {
+        const at::Tensor& t = on.dense(a[5], at::kFloat, "bias float32, dense");
+        need(t.numel() == channels, "bias [channels]");
+        bias = (const float*)t.data_ptr();
+    }
+    const rh_state_rows rows = rows_of(on, a[6], a[4], a[7], a[8], x.size(0), state.size(0));
+    const bool silu = truth(a[9], "silu");
+    const at::Tensor out = given(a[10]) ? as(on, a[10], x, "out as x") : fresh(x.sizes(), x, x.scalar_type());
+    need(!given(a[10]) || apart(out, x), "out apart from x");
+    const rh_status st = f_conv(on.handle, &rows, x.data_ptr(), row_stride(x), (const float*)weight.data_ptr(), bias, type_of(x), channels, width, silu, state.data_ptr(),
+                                out.data_ptr(), row_stride(out));
+    if (st != RH_OK) return status(st);
+    return wrap(out);
+    END
+}
+
+// state_scan(ctx, x, dt, a, b, c, state, slots, skip, gate, dt_bias, softplus, offsets, past, into, out) -> out
+static PyObject* state_scan(PyObject*, PyObject* const* a, Py_ssize_t nargs)
+{
+    BEGIN
+    need(nargs == 16, "sixteen arguments");
+    const context on(a[0]);
+    const at::Tensor& x = on.tensor(a[1], "x on the GPU");
+    need(x.dim() == 2 && x.stride(1) == 1, "x [rows, channels], elements side by side");
+    const at::Tensor &dt = as(on, a[2], x, "dt as x"), &fade = on.dense(a[3], at::kFloat, "a float32, dense"), &state = on.dense(a[6], at::kFloat, "state float32, dense");
+    rh_scan_inputs in = {};
+    in.type = type_of(x); in.channels = fits(x.size(1), "channels");
+    need(fade.dim() == 2 && fade.size(0) == in.channels, "a [channels, n]");
+    in.n = fits(fade.size(1), "n");
+    need(state.dim() == 3 && state.size(1) == in.channels && state.size(2) == in.n, "state [n_slots, channels, n]");
+    const at::Tensor &b = on.tensor(a[4], "b on the GPU"), &c = on.tensor(a[5], "c on the GPU");
+    need(b.dim() == 3 && b.size(0) == x.size(0) && b.size(2) == in.n && c.sizes() == b.sizes() && b.scalar_type() == x.scalar_type() && c.scalar_type() == x.scalar_type(),
+         "b and c alike, [rows, groups, n] of x's type");
+    in.groups = fits(b.size(1), "groups");
+    auto side_by_side = [&](const at::Tensor& t) { return (t.size(2) < 2 || t.stride(2) == 1) && (t.size(1) < 2 || t.stride(1) == t.size(2)); };
+    need(side_by_side(b) && side_by_side(c), "the elements of a row of b and of c side by side");
+    auto wide = [&](const at::Tensor& t) { return t.size(0) > 1 ? t.stride(0) : (int64_t)in.groups * in.n; };
+    auto per_channel = [&](PyObject* o, const char* why) -> const float* {
+        if (!given(o)) return nullptr;
+        const at::Tensor& t = on.dense(o, at::kFloat, why);
+        need(t.numel() == in.channels, why);
+        return (const float*)t.data_ptr();
+    };
+    in.x = x.data_ptr(); in.dt = dt.data_ptr(); in.b = b.data_ptr(); in.c = c.data_ptr(); in.a = (const float*)fade.data_ptr();
+    in.x_stride = row_stride(x); in.dt_stride = row_stride(dt); in.b_stride = wide(b); in.c_stride = wide(c);
+    in.skip = per_channel(a[8], "skip float32 [channels], dense"); in.dt_bias = per_channel(a[10], "dt_bias float32 [channels], dense");
+    const at::Tensor* gate = given(a[9]) ? &as(on, a[9], x, "gate as x") : nullptr;
+    if (gate) { in.gate = gate->data_ptr(); in.gate_stride = row_stride(*gate); }
+    in.softplus = truth(a[11], "softplus");
+    const rh_state_rows rows = rows_of(on, a[12], a[7], a[13], a[14], x.size(0), state.size(0));
+    const at::Tensor out = given(a[15]) ? as(on, a[15], x, "out as x") : fresh(x.sizes(), x, x.scalar_type());
+    need(!given(a[15]) || (apart(out, x) && apart(out, dt) && (!gate || apart(out, *gate))), "out apart from x, dt and gate");
+    const rh_status st = f_scan(on.handle, &rows, &in, (float*)state.data_ptr(), out.data_ptr(), row_stride(out));
+    if (st != RH_OK) return status(st);
+    return wrap(out);
+    END
+}
+
+// norm_gated(ctx, x, gate, weight, groups, eps, outputs) -> (y, y8, y8_scale), None where not asked for
+static PyObject* norm_gated(PyObject*, PyObject* const* a, Py_ssize_t nargs)
+{
+    BEGIN
+    need(nargs == 7, "seven arguments");
+    const context on(a[0]);
+    const at::Tensor &x = on.tensor(a[1], "x on the GPU"), &weight = on.dense(a[3], at::kFloat, "weight float32, dense");
+    need(x.dim() == 2 && x.stride(1) == 1 && weight.numel() == x.size(1), "x [rows, cols], elements side by side, and a weight for every column");
+    const at::Tensor& gate = as(on, a[2], x, "gate as x");
+    const int32_t rows = fits(x.size(0), "x"), cols = fits(x.size(1), "x"), groups = word(a[4], "groups");
+    const double eps = PyFloat_AsDouble(a[5]);
+    need(!PyErr_Occurred(), "eps");
+    const kinds out(a[6]);
+    at::Tensor y, y8, scale;
+    if (out.plain) y = fresh(x.sizes(), x, x.scalar_type());
+    if (out.quantised) { y8 = fresh(x.sizes(), x, at::kFloat8_e4m3fn); scale = fresh({rows}, x, at::kFloat); }
+    auto at_ = [](const at::Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; };
+    const rh_status st = f_gated(on.handle, x.data_ptr(), row_stride(x), gate.data_ptr(), row_stride(gate), (const float*)weight.data_ptr(), type_of(x), rows, cols, groups,
+                                 (float)eps, at_(y), (uint8_t*)at_(y8), (float*)at_(scale));
+    if (st != RH_OK) return status(st);
+    return tuple_of({wrap(y), wrap(y8), wrap(scale)});
+    END
+}
+
+// init(plan, write, attend, norm, matvec, conv, scan, gated): addresses of the library's functions
 static PyObject* init(PyObject*, PyObject* const* a, Py_ssize_t n)
 {
     BEGIN
-    need(n == 5, "five addresses");
+    need(n == 8, "eight addresses");
     f_plan = (decltype(f_plan))integer(a[0], "an address"); f_write = (decltype(f_write))integer(a[1], "an address");
     f_attend = (decltype(f_attend))integer(a[2], "an address"); f_norm = (decltype(f_norm))integer(a[3], "an address");
-    f_matvec = (decltype(f_matvec))integer(a[4], "an address");
+    f_matvec = (decltype(f_matvec))integer(a[4], "an address"); f_conv = (decltype(f_conv))integer(a[5], "an address");
+    f_scan = (decltype(f_scan))integer(a[6], "an address"); f_gated = (decltype(f_gated))integer(a[7], "an address");
     Py_RETURN_NONE;
     END
 }
 
 #define METHOD(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
-static PyMethodDef methods[] = {METHOD(kv_desc), METHOD(cache_plan), METHOD(cache_write), METHOD(cache_attend), METHOD(norm_residual), METHOD(matvec_packed), METHOD(init),
-                                {nullptr, nullptr, 0, nullptr}};
+static PyMethodDef methods[] = {METHOD(kv_desc), METHOD(cache_plan), METHOD(cache_write), METHOD(cache_attend), METHOD(norm_residual), METHOD(matvec_packed),
+                                METHOD(state_conv), METHOD(state_scan), METHOD(norm_gated), METHOD(init), {nullptr, nullptr, 0, nullptr}};
 static PyModuleDef module = {PyModuleDef_HEAD_INIT, "_seq", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 PyMODINIT_FUNC PyInit__seq() { return PyModule_Create(&module); }

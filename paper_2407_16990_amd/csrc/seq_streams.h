@@ -1,0 +1,73 @@
+// Rows of streams (rh_state_rows) cut into pieces of work, which workgroups find by themselves: the offsets lie in device memory.
+#pragma once
+#include "seq_common.h"
+
+#define STREAMS_T 256            // threads of the workgroups that do
+
+struct streams_args {
+    const int32_t *offsets, *slots, *into, *past;
+    int32_t n_streams, n_rows, n_slots;
+};
+
+// the rows of stream b: whatever the offsets say, they lie in [0, n_rows)
+__device__ __forceinline__ void streams_rows(const streams_args& r, int b, int32_t& begin, int32_t& end)
+{
+    auto clipped = [&](int32_t v) { return v < 0 ? 0 : v > r.n_rows ? r.n_rows : v; };
+    begin = clipped(r.offsets[b]); end = clipped(r.offsets[b + 1]);
+    if (end < begin) end = begin;
+}
+// the slot that a stream's state is read from, -1 where it is zeros; and the one it goes to, -1 where it goes nowhere
+__device__ __forceinline__ int32_t streams_slot(const streams_args& r, int b)
+{
+    const int32_t s = r.slots[b];
+    return s < 0 || s >= r.n_slots || (r.past && r.past[b] <= 0) ? -1 : s;
+}
+__device__ __forceinline__ int32_t streams_into(const streams_args& r, int b)
+{
+    const int32_t s = r.into[b];
+    return s < 0 || s >= r.n_slots ? -1 : s;
+}
+
+// For every stream the sum of count(rows) over the streams before it, in s[0 .. n_streams], the last being the sum of all.
+template <typename F>
+__device__ __forceinline__ void streams_sums(const streams_args& r, int32_t* s, int32_t* s_wave, F count)
+{
+    constexpr int PER = RH_SEQ_MAX_STREAMS / STREAMS_T;
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6, per = (r.n_streams + STREAMS_T - 1) / STREAMS_T, b0 = t * per;
+    int32_t n[PER], mine = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        n[i] = 0;
+        if (i >= per || b0 + i >= r.n_streams) continue;
+        int32_t begin, end;
+        streams_rows(r, b0 + i, begin, end);
+        n[i] = count(end - begin);
+        mine += n[i];
+    }
+    int32_t before = seq_scan(mine);
+    if (lane == 63) s_wave[wave] = before;
+    __syncthreads();
+    before -= mine;
+#pragma unroll
+    for (int w = 0; w < STREAMS_T / 64; ++w) if (w < wave) before += s_wave[w];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        if (i >= per || b0 + i >= r.n_streams) continue;
+        s[b0 + i] = before;
+        before += n[i];
+    }
+    if (t == STREAMS_T - 1) s[r.n_streams] = before;         // it has the last streams, or none behind them
+    __syncthreads();
+}
+// Largest b in [0, n) with s[b] <= q; s ascending, s[0] = 0 <= q.
+__device__ __forceinline__ int streams_find(const int32_t* s, int n, int32_t q)
+{
+    int lo = 0;
+    for (int hi = n; hi - lo > 1;) { const int mid = (lo + hi) >> 1; if (s[mid] <= q) lo = mid; else hi = mid; }
+    return lo;
+}
+
+__device__ __forceinline__ float seq_silu(float v) { return v * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(v * -1.44269504089f)); }
+
+// refusals of a call's rows; `name` is the call's
+rh_status streams_check(rh_ctx* ctx, const char* name, const rh_state_rows* r, streams_args* a);
