@@ -1,11 +1,19 @@
 // rh_state_scan: a selective scan of every stream's state over its tokens.  Both types' sources include this.
 //
-// A lane has four of the up to 128 states of a channel, so that LN = 1, 2, 4 ... 32 lanes have a channel's; what they add to y is summed over them by exchanges inside the wave.
-// Single tokens: the states, 2 * 4 * n bytes a channel, are all that counts; a lane loads and stores 16 bytes of them.
-// Many tokens: bound by the vector instructions of h = exp2(delta a) h + delta x b, y += c h: a power of two takes as long as four others.  A
-// workgroup has CH channels of a stream and goes through its rows, SCAN_ROWS of them staged in LDS at a time: delta and delta * x of every
-// channel, worked out once, b and c in fp32; the next rows' loads are in flight meanwhile.  y takes delta's place.
+// Single tokens: the states, 2 * 4 * n bytes a channel, are all that counts.  A lane has four of the up to 128 states of a channel, LN = 1, 2, 4 ... 32
+// neighbouring lanes a channel's, so that a wave loads and stores a stretch of memory; what they add to y is summed over them by exchanges inside the wave.
+//
+// Many tokens: bound by the vector instructions of h = exp2(delta a) h + delta x b, y += c h, of which the power takes twice as long as the four others: 24
+// cycles for a wave's 64 states.  A workgroup has CH channels of a stream and goes through its rows, ROWS of them staged in LDS at a time: delta and delta * x of every
+// channel, worked out once, b and c in fp32; the next rows' loads are in flight meanwhile.  y takes delta's place.  30 streams of 920 rows, 2048
+// channels of 16 states in bf16: 284 us, where the instructions of the recursion alone take 138 and the bytes 89; about a third of the others are softplus and SiLU.
+// Where streams are few, long ones are cut into chunks that are scanned side by side, twice: from zeros, for what they add to the state behind them, and
+// again from the state that those ahead leave.  16384 rows of one stream, 1024 channels: 158 us.
 #pragma once
+#define SCAN_TARGET 4            // workgroups a CU, or so, that streams are cut for
+#define SCAN_LEAST 128           // rows a chunk, at least
+#define SCAN_ROWS 64             // rows a stage, at most
+#define SCAN_WHOLE 0x3FFFFFFF    // rows a chunk that no stream's are one and a half times
 #include "seq_rows.h"
 #include "seq_streams.h"
 
@@ -19,23 +27,24 @@ struct scan_args {
     void* y;
     int64_t x_stride, dt_stride, gate_stride, b_stride, c_stride, y_stride;
     seq_div per, blocks, group_blocks;       // channels a group; workgroups' channel blocks, in all and of a group
+    uint32_t* count;             // a counter for every row of ws and workgroup's block of channels, zero between calls
     int32_t channels, n, softplus, chunk, ws_rows;
 };
 
 // exp(v), off by an ulp or two: the rounding of v * log2(e) is made up for behind the power of two
 __device__ __forceinline__ float scan_exp(float v)
 {
-    const float hi = v * 1.44269504089f, lo = fmaf(v, 1.44269504089f, -hi) + v * 1.92596299e-8f;
+    const float hi = v * 1.44269504089f, lo = fmaf(v, 1.92596299e-8f, fmaf(v, 1.44269504089f, -hi));
     const float e = __builtin_amdgcn_exp2f(hi);
     return fmaf(e, lo * 0.69314718056f, e);
 }
-// log(1 + exp(v)): with w = 1 + e rounded, log(w) * e / (w - 1) makes up for the rounding (Goldberg 1991, theorem 4); above 20 it is v to half an ulp
+// log(1 + exp(v)): with w = 1 + e rounded, log(w) * e / (w - 1) makes up for the rounding (Goldberg 1991, theorem 4); where w is 1 the 2^-100 leave e.
+// Never below v, which it is where e is infinite and the quotient no number.
 __device__ __forceinline__ float scan_softplus(float v)
 {
-    const float e = scan_exp(v), w = 1.f + e, d = w - 1.f;
-    const float l = __builtin_amdgcn_logf(w) * 0.69314718056f;
-    const float s = d == 0.f ? e : l * (e * __builtin_amdgcn_rcpf(d));
-    return v > 20.f ? v : s;
+    const float e = scan_exp(v), w = 1.f + e;
+    const float l = fmaf(__builtin_amdgcn_logf(w), 0.69314718056f, 0x1p-100f), d = fmaxf(w - 1.f, 0x1p-100f);
+    return fmaxf(l * (e * __builtin_amdgcn_rcpf(d)), v);
 }
 
 // the sum over LN neighbouring lanes, the same for all of them
@@ -49,6 +58,23 @@ template <int LN> __device__ __forceinline__ float scan_over(float v)
     if constexpr (LN >= 32) v += __shfl_xor(v, 16);
     return v;
 }
+// Four rows' values summed over the LN lanes that lie 64 / LN apart, by exchanges that leave half as many values each time: v[i] then has row scan_row(i).
+template <int LN> __device__ __forceinline__ void scan_join(float (&v)[4])
+{
+    auto halves = [](float& x, float& y, auto rows) {        // of x the lower halves (even rows) of both, of y the upper (odd): their sum
+        typedef __attribute__((__vector_size__(2 * sizeof(uint32_t)))) uint32_t two;
+        two r;
+        if constexpr (decltype(rows)::value == 32) r = __builtin_bit_cast(two, __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(y), false, false));
+        else r = __builtin_bit_cast(two, __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(y), false, false));
+        return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    };
+    auto around = [](float x, auto ctrl) { return x + __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), decltype(ctrl)::value, 0xF, 0xF, true)); };
+    if constexpr (LN >= 2) { v[0] = halves(v[0], v[1], seq_const<32>()); v[1] = halves(v[2], v[3], seq_const<32>()); }
+    if constexpr (LN >= 4) v[0] = halves(v[0], v[1], seq_const<16>());
+    if constexpr (LN >= 8) v[0] = around(v[0], seq_const<0x128>());          // 8 lanes around the 16
+    if constexpr (LN >= 16) v[0] = around(v[0], seq_const<0x124>());
+}
+template <int LN> __device__ __forceinline__ int scan_row(int i, int lane) { return LN == 1 ? i : LN == 2 ? 2 * i + (lane >> 5) : (lane >> 4 & 1) * 2 + (lane >> 5); }
 
 // four elements from i on, of n; zeros behind
 template <typename T, bool FULL> __device__ __forceinline__ f32x4 scan_quad(const T* p, int i, int n)
@@ -140,14 +166,12 @@ template <int ROWS> struct scan_cut {
         n = (int32_t)(((uint32_t)len + size - 1) / (uint32_t)size);                         // rounded up to whole stages, fewer may do
     }
 };
-// what a workgroup counts of a stream to find its own: its chunks, those that leave something to the next, or the streams that are cut
-enum { SCAN_ALL, SCAN_SUMS, SCAN_CARRY };
-
 // The stream that the workgroup's index q falls in, its place in it, and the row of ws where the stream's chunks begin; false where there is none.
-template <int ROWS, int WHAT>
-__device__ __forceinline__ bool scan_find(const scan_args& a, int32_t q, int32_t* s_mem, int32_t* s_wave, int& b, int32_t& place, int32_t& row)
+// The first launch has every chunk but the last of the streams that are cut; the second has all streams' chunks.
+template <int ROWS, bool OUT>
+__device__ __forceinline__ bool scan_find(const scan_args& a, int32_t q, int32_t* s_mem, int& b, int32_t& place, int32_t& row)
 {
-    auto own = [&](int32_t len) { const scan_cut<ROWS> k(len, a.chunk); return WHAT == SCAN_ALL ? k.n : k.n < 2 ? 0 : WHAT == SCAN_SUMS ? k.n - 1 : 1; };
+    auto own = [&](int32_t len) { const scan_cut<ROWS> k(len, a.chunk); return OUT ? k.n : k.n < 2 ? 0 : k.n - 1; };
     auto rows = [&](int32_t len) { const scan_cut<ROWS> k(len, a.chunk); return k.n < 2 ? 0 : k.n; };
     if (a.r.n_streams <= 64) {                               // a stream a lane
         const int lane = threadIdx.x & 63;
@@ -160,7 +184,7 @@ __device__ __forceinline__ bool scan_find(const scan_args& a, int32_t q, int32_t
         place = q - __builtin_amdgcn_readlane(upto - mine, b);
         row = __builtin_amdgcn_readlane(ahead, b);
     } else {
-        int32_t* s_rows = s_mem + a.r.n_streams + 1;
+        int32_t *s_rows = s_mem + a.r.n_streams + 1, *s_wave = s_rows + a.r.n_streams + 1;
         streams_sums(a.r, s_mem, s_wave, own);
         streams_sums(a.r, s_rows, s_wave, rows);
         if (q >= s_mem[a.r.n_streams]) return false;
@@ -171,255 +195,306 @@ __device__ __forceinline__ bool scan_find(const scan_args& a, int32_t q, int32_t
     return place >= 0;
 }
 
-template <typename T, int LN, int K> struct scan_shape {
-    static constexpr int E = 16 / sizeof(T), CH = 256 / LN * K;
-    static constexpr int BY_X = 4096 / CH, BY_B = 1024 / LN, MOST = 64;
+#define SCAN_AHEAD 8             // chunks whose states and sums are in flight
+// LN lanes have a channel's states, NS each; E: elements of 16 bytes.
+template <typename T, int LN, int NS> struct scan_shape {
+    static constexpr int E = 16 / sizeof(T), N = LN * NS, WCH = 64 / LN, CH = 4 * WCH;           // WCH: channels of a wave
+    static constexpr int BY_X = 4096 / CH, BY_B = 4096 / N, MOST = SCAN_ROWS;
     static constexpr int ROWS = (BY_X < BY_B ? BY_X : BY_B) < MOST ? (BY_X < BY_B ? BY_X : BY_B) : MOST;     // 32 KB of LDS for delta and delta * x, or for b and c, at most
     static constexpr int PIECES = ROWS * CH / E, NX = (PIECES + 255) / 256;              // of 16 bytes of x, a stage's and a thread's
-    static constexpr int QUADS = ROWS * LN, NB = (QUADS + 255) / 256;                    // of b, and of c
-    static constexpr int LDS = ROWS * (CH * 2 + LN * 8) * 4;
+    static constexpr int QUADS = ROWS * N / 4, NB = (QUADS + 255) / 256;                 // of b, and of c
+    static constexpr int LDS = ROWS * (CH + N) * 2 * 4;
 };
 
-// OUT: y and the states behind the streams' last rows.  Otherwise what a chunk makes of a state of zeros, and the sum of its delta, for the next one.
-template <typename T, int LN, int K, bool FULL, bool OUT>
-__global__ __launch_bounds__(256) void k_seq_scan(scan_args a)
+// One workgroup's rows of one stream, [first, stop), and CH channels, block blk of them.  OUT: y, and the state behind the stream's last row.  Otherwise what a chunk
+// makes of a state of zeros and the sum of its delta; the stream's last such chunk to finish then works out the states that its chunks begin with.
+// Lane l of a wave has the states NS * (l / WCH) + ... of the channels l % WCH + ...  The product delta x b goes on the matrix cores, whose 4x4x1 product
+// adds to the four states of each of a block's four lanes (channels) the four elements of b times the lane's delta * x: 1 instruction for 4 fused ones and 4 products.
+template <typename T, int LN, int NS, bool FULL, bool OUT>
+__device__ __forceinline__ void scan_chunk(const scan_args& a, f32x4* s_stage, int b, int32_t place, int32_t ws_row, int32_t chunks, int32_t blk, int32_t first, int32_t stop)
 {
-    typedef scan_shape<T, LN, K> S;
-    constexpr int E = S::E, CH = S::CH, ROWS = S::ROWS, NX = S::NX, NB = S::NB, LW = LN < 4 ? LN : 4;
-    extern __shared__ f32x4 s_stage[];
-    __shared__ int32_t s_wave[STREAMS_T / 64];
+    typedef scan_shape<T, LN, NS> S;
+    constexpr int E = S::E, CH = S::CH, WCH = S::WCH, N = S::N, ROWS = S::ROWS, NX = S::NX, NB = S::NB, Q = NS / 4;
     float* s_du = (float*)s_stage;                           // [row][channel]: delta and delta * x, then y
-    f32x4 *s_b = (f32x4*)(s_du + ROWS * CH * 2), *s_c = s_b + ROWS * LN;
+    float *s_b = s_du + ROWS * CH * 2, *s_c = s_b + ROWS * N;
+    int32_t* s_odd = (int32_t*)(s_c + ROWS * N);             // unless FULL: whether any delta * x of the rows in LDS is not finite; of the next ones
 
-    const int t = threadIdx.x, j = t % LN, cl = t / LN * K;
-    const uint32_t item = seq_quot(blockIdx.x, a.blocks), blk = blockIdx.x - item * a.blocks.d;
-    int b;
-    int32_t place, ws_row;
-    if (!scan_find<ROWS, OUT ? SCAN_ALL : SCAN_SUMS>(a, (int32_t)item, (int32_t*)s_stage, s_wave, b, place, ws_row)) return;
-    int32_t begin, end;
-    streams_rows(a.r, b, begin, end);
-    const scan_cut<ROWS> cut(end - begin, a.chunk);
-    if (place >= cut.n || (cut.n > 1 && ws_row + cut.n > a.ws_rows)) return;                // offsets that do not ascend
-    const int32_t first = begin + place * cut.size, stop = end - first < cut.size ? end : first + cut.size;
-    const int g = (int)seq_quot(blk, a.group_blocks);
-    const int c_end = (g + 1) * (int)a.per.d, c_blk = g * (int)a.per.d + (int)(blk - (uint32_t)g * a.group_blocks.d) * CH;       // the group's last channel + 1, this block's first
+    const int t = threadIdx.x, lane = t & 63, cl = (t >> 6) * WCH + lane % WCH, n0 = lane / WCH * NS;
+    const int g = (int)seq_quot((uint32_t)blk, a.group_blocks);
+    const int c_end = (g + 1) * (int)a.per.d, c_blk = g * (int)a.per.d + (blk - g * (int)a.group_blocks.d) * CH;         // the group's last channel + 1, this block's first
     const int64_t pool = (int64_t)a.channels * a.n;
-    float* sums = a.ws + (int64_t)a.ws_rows * a.channels * (4 * LN);
+    float* sums = a.ws + (int64_t)a.ws_rows * a.channels * N;
 
-    // ---- this lane's states
-    f32x4 h[K], fade[K];
-    float total[K];
+    // ---- this lane's states, of channel cs (of the last one, and of no account, where the group has no more)
+    const int cs = c_blk + cl < c_end ? c_blk + cl : c_end - 1;
+    const bool mine = c_blk + cl < c_end;
+    const int64_t at = (int64_t)cs * a.n;
+    f32x4 h[Q], fade[Q];
+    float total = 0.f;
     {
-        const int32_t from = cut.n < 2 ? streams_slot(a.r, b) : -1;
+        const int32_t from = chunks < 2 ? streams_slot(a.r, b) : -1;
 #pragma unroll
-        for (int k = 0; k < K; ++k) {
-            const int c = c_blk + cl + k < c_end ? c_blk + cl + k : c_end - 1;
-            fade[k] = scan_quad<float, FULL>(a.a + (int64_t)c * a.n, 4 * j, a.n) * 1.44269504089f;
-            h[k] = f32x4{0.f, 0.f, 0.f, 0.f};
-            total[k] = 0.f;
-            if (OUT && cut.n > 1) h[k] = *(const f32x4*)(a.ws + ((int64_t)(ws_row + place) * a.channels + c) * (4 * LN) + 4 * j);
-            else if (OUT && from >= 0) h[k] = scan_quad<float, FULL>(a.state + from * pool + (int64_t)c * a.n, 4 * j, a.n);
+        for (int q = 0; q < Q; ++q) {
+            const int n = n0 + 4 * q;
+            fade[q] = scan_quad<float, FULL>(a.a + at, n, a.n) * 1.44269504089f;
+            h[q] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if (OUT && chunks > 1) h[q] = *(const f32x4*)(a.ws + ((int64_t)(ws_row + place) * a.channels + cs) * N + n);
+            else if (OUT && from >= 0) h[q] = scan_quad<float, FULL>(a.state + from * pool + at, n, a.n);
         }
     }
 
     // ---- this thread's pieces of the rows: E channels, the same of every row that it has
-    constexpr int PR = CH / E;                               // pieces a row
-    const int pc = t % PR * E, pr = t / PR, cg = c_blk + pc, left = c_end - cg;
+    constexpr int PR = CH / E, RX = 256 / PR, RB = 256 / (N / 4);            // pieces a row; rows from a thread's piece, or quad of b, to its next
+    const int pc = t % PR * E, pr = t / PR, cg = c_blk + pc, left = c_end - cg, br = t / (N / 4), bn = t % (N / 4) * 4;
+    const bool narrow = c_end < E, whole = c_blk + CH <= c_end;              // fewer channels than a piece; no piece that is not a whole one
+    const int cc = narrow ? 0 : cg < c_end - E ? cg : c_end - E;             // where it is loaded from
     float bias[E], skip[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) {
         bias[e] = a.dt_bias && e < left ? a.dt_bias[cg + e] : 0.f;
         skip[e] = OUT && a.skip && e < left ? a.skip[cg + e] : 0.f;
     }
+    // where its first piece of a stage's rows lies, and its first quad
+    const T *px = (const T*)a.x + (int64_t)(first + pr) * a.x_stride + cc, *pd = (const T*)a.dt + (int64_t)(first + pr) * a.dt_stride + cc;
+    const T *pz = (const T*)a.gate + (int64_t)(first + pr) * a.gate_stride + cc;
+    const T *pb = (const T*)a.b + (int64_t)(first + br) * a.b_stride + (int64_t)g * a.n, *pq = (const T*)a.c + (int64_t)(first + br) * a.c_stride + (int64_t)g * a.n;
+    T* py = (T*)a.y + (int64_t)(first + pr) * a.y_stride + cg;
     struct raw { u32x4 x[NX], dt[NX]; f32x4 b[NB], c[NB]; };
     u32x4 gate[NX];
-    auto load = [&](int32_t row, raw& in) __attribute__((always_inline)) {
+    auto piece = [&](const T* p) __attribute__((always_inline)) { return narrow ? row_load<T, E>(p, cg, c_end) : seq_load<u32x4>(p); };
+    auto value = [&](u32x4 w, float (&v)[E]) __attribute__((always_inline)) {
+        if (whole) row_place<T, E>(w, 0, E, v); else row_place<T, E>(w, cg, c_end, v);
+    };
+    // the thread's pieces (quads) of a stage: those of rows that are there; where some are not, behind the last, of the last
+    auto each = [&](auto n, auto step, int r0, bool full, int rows, auto f) __attribute__((always_inline)) {
+        if (full) {
 #pragma unroll
-        for (int i = 0; i < NX; ++i) {
-            const int r = i * (256 / PR) + pr;
-            const int64_t at = row + r < stop ? row + r : stop - 1;
-            if (S::PIECES < 256 && r >= ROWS) { in.x[i] = in.dt[i] = u32x4{0, 0, 0, 0}; continue; }
-            in.x[i] = row_load<T, E>((const T*)a.x + at * a.x_stride, cg, c_end);
-            in.dt[i] = row_load<T, E>((const T*)a.dt + at * a.dt_stride, cg, c_end);
-        }
+            for (int i = 0; i < decltype(n)::value; ++i) f(i, i * decltype(step)::value);
+        } else {
 #pragma unroll
-        for (int i = 0; i < NB; ++i) {
-            const int q = i * 256 + t, r = q / LN;
-            const int64_t at = row + r < stop ? row + r : stop - 1;
-            in.b[i] = scan_quad<T, FULL>((const T*)a.b + at * a.b_stride + (int64_t)g * a.n, 4 * (q % LN), a.n);
-            if (OUT) in.c[i] = scan_quad<T, FULL>((const T*)a.c + at * a.c_stride + (int64_t)g * a.n, 4 * (q % LN), a.n);
+            for (int i = 0; i < decltype(n)::value; ++i) f(i, (i * decltype(step)::value + r0 < rows ? i * decltype(step)::value + r0 : rows - 1) - r0);
         }
     };
+    const seq_const<NX> nx; const seq_const<NB> nb; const seq_const<RX> rx; const seq_const<RB> rb;
+    constexpr bool IDLE = S::PIECES < 256, IDLE_B = S::QUADS < 256;          // threads without a piece, without a quad
     raw in;
-    load(first, in);
-    if (a.r.n_streams > 64) __syncthreads();                 // the counts there have been read
-    for (int32_t row = first; row < stop; row += ROWS) {
-        const int rows = stop - row < ROWS ? stop - row : ROWS;
+    auto load = [&](int rows) __attribute__((always_inline)) {
+        if (!IDLE || pr < ROWS) each(nx, rx, pr, rows >= ROWS, rows, [&](int i, int r) { in.x[i] = piece(px + r * a.x_stride); in.dt[i] = piece(pd + r * a.dt_stride); });
+        if (!IDLE_B || br < ROWS) each(nb, rb, br, rows >= ROWS, rows, [&](int i, int r) {
+            in.b[i] = scan_quad<T, FULL>(pb + r * a.b_stride, bn, a.n);
+            if (OUT) in.c[i] = scan_quad<T, FULL>(pq + r * a.c_stride, bn, a.n);
+        });
+        px += ROWS * a.x_stride; pd += ROWS * a.dt_stride; pb += ROWS * a.b_stride; pq += ROWS * a.c_stride;
+    };
+    load(stop - first);
+    if (a.r.n_streams > 64) __syncthreads();                 // the counts in LDS have been read
+    if (!FULL) {
+        if (t < 2) s_odd[t] = 0;
+        __syncthreads();
+    }
+    int turn = 0;
+    for (int32_t row = first; row < stop; row += ROWS, turn ^= 1) {
+        const int rows = stop - row;                         // and those behind the stage's
+        const bool full = rows >= ROWS;
         // ---- into LDS; rows behind the last leave the state as it is: delta, delta * x and b are zero
-        float x[NX][E];
+        u32x4 kept[NX];                                      // x, for the skip
+        if (!IDLE || pr < ROWS) {
+            bool odd = false;
 #pragma unroll
-        for (int i = 0; i < NX; ++i) {
-            const int r = i * (256 / PR) + pr;
-            float dt[E];
-            row_place<T, E>(in.x[i], cg, c_end, x[i]);
-            row_place<T, E>(in.dt[i], cg, c_end, dt);
-            if (S::PIECES < 256 && r >= ROWS) continue;
-            float* to = s_du + (r * CH + pc) * 2;
+            for (int i = 0; i < NX; ++i) {
+                float x[E], dt[E];
+                if (OUT) kept[i] = in.x[i];
+                value(in.x[i], x);
+                value(in.dt[i], dt);
 #pragma unroll
-            for (int e = 0; e < E; e += 2) {
-                f32x4 v;
+                for (int e = 0; e < E; ++e) dt[e] += bias[e];
+                if (a.softplus) {
 #pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    float d = dt[e + k] + bias[e + k];
-                    d = a.softplus ? scan_softplus(d) : d;
-                    v[2 * k] = r < rows ? d : 0.f;
-                    v[2 * k + 1] = r < rows ? d * x[i][e + k] : 0.f;
+                    for (int e = 0; e < E; ++e) dt[e] = scan_softplus(dt[e]);
                 }
-                *(f32x4*)(to + 2 * e) = v;
+                f32x4* to = (f32x4*)(s_du + ((i * RX + pr) * CH + pc) * 2);
+#pragma unroll
+                for (int e = 0; e < E; e += 2) {
+                    const f32x4 v = {dt[e], dt[e] * x[e], dt[e + 1], dt[e + 1] * x[e + 1]};
+                    if (!FULL) odd |= !(fabsf(v[1]) < INFINITY) || !(fabsf(v[3]) < INFINITY);
+                    to[e / 2] = v;
+                }
             }
+            if (!FULL && odd) s_odd[turn] = 1;
         }
 #pragma unroll
         for (int i = 0; i < NB; ++i) {
-            const int q = i * 256 + t, r = q / LN;
-            if (S::QUADS % 256 && q >= S::QUADS) continue;
-            s_b[q] = r < rows ? in.b[i] : f32x4{0.f, 0.f, 0.f, 0.f};
-            if (OUT) s_c[q] = in.c[i];
+            if (IDLE_B && br >= ROWS) break;
+            *(f32x4*)(s_b + (i * RB + br) * N + bn) = in.b[i];
+            if (OUT) *(f32x4*)(s_c + (i * RB + br) * N + bn) = in.c[i];
+        }
+        if (!full) {
+#pragma unroll
+            for (int i = 0; i < NX; ++i)
+                if (i * RX + pr >= rows && (!IDLE || pr < ROWS))
+#pragma unroll
+                    for (int e = 0; e < E; e += 2) ((f32x4*)(s_du + ((i * RX + pr) * CH + pc) * 2))[e / 2] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < NB; ++i)
+                if (i * RB + br >= rows && (!IDLE_B || br < ROWS)) *(f32x4*)(s_b + (i * RB + br) * N + bn) = f32x4{0.f, 0.f, 0.f, 0.f};
         }
         __syncthreads();
         // ---- the next rows' loads, and these rows' gate
         if (OUT && a.gate) {
-#pragma unroll
-            for (int i = 0; i < NX; ++i) {
-                const int r = i * (256 / PR) + pr;
-                if (S::PIECES < 256 && r >= ROWS) continue;
-                const int64_t at = row + r < stop ? row + r : stop - 1;
-                gate[i] = row_load<T, E>((const T*)a.gate + at * a.gate_stride, cg, c_end);
-            }
+            if (!IDLE || pr < ROWS) each(nx, rx, pr, full, rows, [&](int i, int r) { gate[i] = piece(pz + r * a.gate_stride); });
+            pz += ROWS * a.gate_stride;
         }
-        if (row + ROWS < stop) load(row + ROWS, in);
+        if (rows > ROWS) load(rows - ROWS);
         // ---- the rows
-        for (int r0 = 0; r0 < rows; r0 += 4) {
-            float mine[K][4 / LW];
+        auto four = [&](int r0, auto masked) __attribute__((always_inline)) {
+            float y[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int r = r0 + i;
-                const f32x4 bq = s_b[r * LN + j], cq = OUT ? s_c[r * LN + j] : f32x4{0.f, 0.f, 0.f, 0.f};
-                float du[2 * K];
+                const float2 du = *(const float2*)(s_du + (r * CH + cl) * 2);
+                float sum = 0.f;
 #pragma unroll
-                for (int k = 0; k < 2 * K; k += 2) {
-                    if constexpr (K % 2 == 0) {
-                        if (k % 4 == 0) { const f32x4 v = *(const f32x4*)(s_du + (r * CH + cl) * 2 + k); du[k] = v[0]; du[k + 1] = v[1]; du[k + 2] = v[2]; du[k + 3] = v[3]; }
-                    } else { const float2 v = *(const float2*)(s_du + (r * CH + cl) * 2 + k); du[k] = v.x; du[k + 1] = v.y; }
-                }
+                for (int q = 0; q < Q; ++q) {
+                    const float bq = s_b[r * N + n0 + 4 * q + lane % 4];
+                    f32x4 v;
 #pragma unroll
-                for (int k = 0; k < K; ++k) {
-                    float y = 0.f;
+                    for (int e = 0; e < 4; ++e) v[e] = h[q][e] * __builtin_amdgcn_exp2f(du.x * fade[q][e]);
+                    v = __builtin_amdgcn_mfma_f32_4x4x1f32(bq, du.y, v, 0, 0, 0);
+                    if constexpr (decltype(masked)::value) {                // states that are none: an infinite delta * x times their zero
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        h[k][e] = fmaf(__builtin_amdgcn_exp2f(du[2 * k] * fade[k][e]), h[k][e], du[2 * k + 1] * bq[e]);
-                        if (!FULL && 4 * j + e >= a.n) h[k][e] = 0.f;       // an infinite delta * x times the zero there
-                        if (OUT) y = e ? fmaf(cq[e], h[k][e], y) : cq[e] * h[k][e];
+                        for (int e = 0; e < 4; ++e) if (n0 + 4 * q + e >= a.n) v[e] = 0.f;
                     }
                     if constexpr (OUT) {
-                        y = scan_over<LN>(y);
-                        mine[k][i / LW] = i % LW == 0 || i % LW == j % LW ? y : mine[k][i / LW];
-                    } else total[k] += du[2 * k];
+                        const f32x4 cq = *(const f32x4*)(s_c + r * N + n0 + 4 * q);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) sum = q + e ? fmaf(cq[e], v[e], sum) : cq[e] * v[e];
+                    }
+                    h[q] = v;
                 }
+                y[i] = sum;
+                if (!OUT) total += du.x;
             }
-            if (OUT && j < LW) {
+            if constexpr (OUT) {
+                scan_join<LN>(y);
 #pragma unroll
-                for (int i = 0; i < 4 / LW; ++i)
-#pragma unroll
-                    for (int k = 0; k < K; ++k) s_du[((r0 + i * LW + j % LW) * CH + cl + k) * 2] = mine[k][i];
+                for (int i = 0; i < (LN < 4 ? 4 / LN : 1); ++i) s_du[((r0 + scan_row<LN>(i, lane)) * CH + cl) * 2] = y[i];
             }
-        }
+        };
+        const int some = full ? ROWS : rows;
+        if (!FULL && s_odd[turn]) for (int r0 = 0; r0 < some; r0 += 4) four(r0, seq_const<1>());
+        else for (int r0 = 0; r0 < some; r0 += 4) four(r0, seq_const<0>());
         __syncthreads();
+        if (!FULL && t == 0) s_odd[turn] = 0;                // the rows after the next write it again, behind a barrier
         // ---- y: the thread's own pieces, which it also fills with the next rows
         if constexpr (OUT) {
 #pragma unroll
             for (int i = 0; i < NX; ++i) {
-                const int r = i * (256 / PR) + pr;
-                if (r >= rows) continue;
+                if (i * RX + pr >= some) continue;
                 float y[E], z[E];
+                const f32x4* from = (const f32x4*)(s_du + ((i * RX + pr) * CH + pc) * 2);
 #pragma unroll
-                for (int e = 0; e < E; e += 2) {
-                    const f32x4 v = *(const f32x4*)(s_du + (r * CH + pc + e) * 2);
-                    y[e] = v[0]; y[e + 1] = v[2];
+                for (int e = 0; e < E; e += 2) { y[e] = from[e / 2][0]; y[e + 1] = from[e / 2][2]; }
+                if (a.skip) {
+                    value(kept[i], z);
+#pragma unroll
+                    for (int e = 0; e < E; ++e) y[e] = fmaf(skip[e], z[e], y[e]);
                 }
-                if (a.skip)
-#pragma unroll
-                    for (int e = 0; e < E; ++e) y[e] = fmaf(skip[e], x[i][e], y[e]);
                 if (a.gate) {
-                    row_place<T, E>(gate[i], cg, c_end, z);
+                    value(gate[i], z);
 #pragma unroll
                     for (int e = 0; e < E; ++e) y[e] *= seq_silu(z[e]);
                 }
-                if (left > 0) row_store<T, E>((T*)a.y + (int64_t)(row + r) * a.y_stride + cg, left, y);
+                if (whole) row_store<T, E>(py + i * RX * a.y_stride, E, y);
+                else if (left > 0) row_store<T, E>(py + i * RX * a.y_stride, left, y);
+            }
+            py += ROWS * a.y_stride;
+        }
+    }
+    if constexpr (OUT) {                                     // ---- the state behind the last row
+        const int32_t to = place == chunks - 1 ? streams_into(a.r, b) : -1;
+        if (to < 0 || !mine) return;
+#pragma unroll
+        for (int q = 0; q < Q; ++q) scan_put<FULL>(a.state + to * pool + at, n0 + 4 * q, a.n, h[q]);
+    } else {
+        // ---- what the chunk leaves.  The chunks of a stream sit on eight XCDs with an L2 each: stored through with relaxed atomics of the device's scope, loaded past
+        // the L2 by the one that finishes last, and acknowledged before the chunk is counted.
+        struct two { uint64_t u[2]; };
+        auto state_at = [&](int32_t chunk, int q) {          // a row's place is the same for all lanes, theirs in it 32 bits
+            return (float*)((char*)(a.ws + (int64_t)(ws_row + chunk) * a.channels * N) + (uint32_t)((cs * N + n0 + 4 * q) * 4));
+        };
+        auto sum_at = [&](int32_t chunk) { return (uint32_t*)((char*)(sums + (int64_t)(ws_row + chunk) * a.channels) + (uint32_t)(cs * 4)); };
+        if (mine) {
+#pragma unroll
+            for (int q = 0; q < Q; ++q) {
+                const two w = __builtin_bit_cast(two, h[q]);
+                uint64_t* p = (uint64_t*)state_at(place, q);
+                __hip_atomic_store(p, w.u[0], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                __hip_atomic_store(p + 1, w.u[1], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            }
+            if (n0 == 0) __hip_atomic_store(sum_at(place), __float_as_uint(total), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        int32_t* s_last = (int32_t*)s_stage;                 // what LDS held has been read
+        __syncthreads();
+        if (t == 0) {
+            uint32_t* count = a.count + (int64_t)ws_row * a.blocks.d + blk;
+            const bool last = __hip_atomic_fetch_add(count, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)chunks - 2;
+            if (last) __hip_atomic_store(count, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            *s_last = last;
+        }
+        __syncthreads();
+        if (!*s_last || !mine) return;
+        // ---- h = exp(a * sum of delta) h + what the chunk makes of zeros, chunk after chunk, in the place of the latter: the states that chunks begin with
+        const int32_t from = streams_slot(a.r, b);
+#pragma unroll
+        for (int q = 0; q < Q; ++q) {
+            f32x4 v = {0.f, 0.f, 0.f, 0.f};
+            if (from >= 0) v = scan_quad<float, FULL>(a.state + from * pool + at, n0 + 4 * q, a.n);
+            for (int32_t c0 = 0; c0 < chunks; c0 += SCAN_AHEAD) {
+                two add[SCAN_AHEAD];
+                uint32_t sum[SCAN_AHEAD];
+#pragma unroll
+                for (int i = 0; i < SCAN_AHEAD; ++i) {
+                    const int32_t k = c0 + i < chunks - 1 ? c0 + i : 0;                  // the last chunk leaves nothing
+                    const uint64_t* p = (const uint64_t*)state_at(k, q);
+                    add[i].u[0] = __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                    add[i].u[1] = __hip_atomic_load(p + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                    sum[i] = __hip_atomic_load(sum_at(k), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                }
+#pragma unroll
+                for (int i = 0; i < SCAN_AHEAD; ++i) {
+                    if (c0 + i >= chunks) break;
+                    *(f32x4*)state_at(c0 + i, q) = v;
+                    const f32x4 more = __builtin_bit_cast(f32x4, add[i]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[e] = fmaf(__builtin_amdgcn_exp2f(__uint_as_float(sum[i]) * fade[q][e]), v[e], more[e]);
+                }
             }
         }
     }
-    // ---- the state behind the last row
-    const int32_t to = OUT && place == cut.n - 1 ? streams_into(a.r, b) : -1;
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-        const int c = c_blk + cl + k;
-        if (c >= c_end) continue;
-        if (!OUT) {
-            const int64_t at = (int64_t)(ws_row + place) * a.channels + c;
-            *(f32x4*)(a.ws + at * (4 * LN) + 4 * j) = h[k];
-            if (j == 0) sums[at] = total[k];
-        } else if (to >= 0) scan_put<FULL>(a.state + to * pool + (int64_t)c * a.n, 4 * j, a.n, h[k]);
-    }
 }
 
-// The states that the chunks of the cut streams begin with, in the place of what each makes of zeros: h = exp(a * sum of delta) h + that, chunk after chunk.
-#define SCAN_AHEAD 8             // chunks whose loads are in flight
-template <int LN, int ROWS, bool FULL>
-__global__ __launch_bounds__(256) void k_seq_scan_carry(scan_args a)
+template <typename T, int LN, int NS, bool FULL, bool OUT>
+__global__ __launch_bounds__(256, 2) void k_seq_scan(scan_args a)
 {
+    constexpr int ROWS = scan_shape<T, LN, NS>::ROWS;
     extern __shared__ f32x4 s_stage[];
-    __shared__ int32_t s_wave[STREAMS_T / 64];
+    const uint32_t item = seq_quot(blockIdx.x, a.blocks), blk = blockIdx.x - item * a.blocks.d;
     int b;
-    int32_t place, ws_row;
-    const uint32_t item = seq_quot(blockIdx.x, a.blocks);
-    if (!scan_find<ROWS, SCAN_CARRY>(a, (int32_t)item, (int32_t*)s_stage, s_wave, b, place, ws_row)) return;
-    int32_t begin, end;
+    int32_t place, ws_row, begin, end;
+    if (!scan_find<ROWS, OUT>(a, (int32_t)item, (int32_t*)s_stage, b, place, ws_row)) return;
     streams_rows(a.r, b, begin, end);
     const scan_cut<ROWS> cut(end - begin, a.chunk);
-    if (place > 0 || cut.n < 2 || ws_row + cut.n > a.ws_rows) return;
-    const int c = (int)(blockIdx.x - item * a.blocks.d) * (256 / LN) + threadIdx.x / LN, j = threadIdx.x % LN;
-    if (c >= a.channels) return;
-    const int32_t from = streams_slot(a.r, b);
-    const f32x4 fade = scan_quad<float, FULL>(a.a + (int64_t)c * a.n, 4 * j, a.n) * 1.44269504089f;
-    f32x4 h = {0.f, 0.f, 0.f, 0.f};
-    if (from >= 0) h = scan_quad<float, FULL>(a.state + (int64_t)from * a.channels * a.n + (int64_t)c * a.n, 4 * j, a.n);
-    const int64_t step = (int64_t)a.channels * (4 * LN);
-    float* at = a.ws + ((int64_t)ws_row * a.channels + c) * (4 * LN) + 4 * j;
-    const float* sum = a.ws + (int64_t)a.ws_rows * step + (int64_t)ws_row * a.channels + c;
-    for (int32_t k0 = 0; k0 < cut.n; k0 += SCAN_AHEAD) {
-        f32x4 add[SCAN_AHEAD];
-        float total[SCAN_AHEAD];
-#pragma unroll
-        for (int i = 0; i < SCAN_AHEAD; ++i) {
-            const int32_t k = k0 + i < cut.n - 1 ? k0 + i : 0;               // the last chunk leaves nothing
-            add[i] = *(const f32x4*)(at + k * step);
-            total[i] = sum[(int64_t)k * a.channels];
-        }
-#pragma unroll
-        for (int i = 0; i < SCAN_AHEAD; ++i) {
-            if (k0 + i >= cut.n) break;
-            *(f32x4*)(at + (k0 + i) * step) = h;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) h[e] = fmaf(__builtin_amdgcn_exp2f(total[i] * fade[e]), h[e], add[i][e]);
-        }
-    }
+    if (place >= cut.n || (cut.n > 1 && ws_row + cut.n > a.ws_rows)) return;             // offsets that do not ascend
+    const int32_t first = begin + place * cut.size, stop = end - first < cut.size ? end : first + cut.size;
+    scan_chunk<T, LN, NS, FULL, OUT>(a, s_stage, b, place, ws_row, cut.n, (int32_t)blk, first, stop);
 }
 
 template <typename T, int LN, bool FULL>
 static hipError_t launch_scan(rh_ctx* ctx, scan_args& a, rh_status* failed)
 {
-    constexpr int K = 2;
-    typedef scan_shape<T, LN, K> S;
+    constexpr int WL = LN > 16 ? 16 : LN, NS = 4 * LN / WL;
+    typedef scan_shape<T, WL, NS> S;
     const int groups = a.channels / (int)a.per.d;
     const int64_t wide = (a.channels + 256 / LN - 1) / (256 / LN);           // workgroups of one channel a thread
     if (!a.r.offsets) {
@@ -430,36 +505,33 @@ static hipError_t launch_scan(rh_ctx* ctx, scan_args& a, rh_status* failed)
     }
     const int group_blocks = ((int)a.per.d + S::CH - 1) / S::CH;
     const int64_t blocks = (int64_t)groups * group_blocks;
-    // rows a chunk: enough workgroups for the GPU where streams are few, and no more states than the scratch memory holds
-    const int64_t room = SCAN_ROOM(ctx) / ((int64_t)a.channels * (4 * LN + 1));
-    const int64_t least = room > 0 ? (int64_t)a.r.n_rows * 4 / (3 * room) + 1 : 0x3FFFFFFF;
-    int64_t chunk = (int64_t)a.r.n_rows * blocks / (2 * ctx->n_cu);
-    chunk = chunk < 4 * S::ROWS ? 4 * S::ROWS : chunk;
-    chunk = chunk < 128 ? 128 : chunk;
-    chunk = chunk < least ? least : chunk;
-    a.chunk = (int32_t)(chunk > 0x3FFFFFFF ? 0x3FFFFFFF : chunk);
-    const bool cut = 2 * (int64_t)a.r.n_rows >= 3 * (int64_t)a.chunk;        // otherwise no stream can be as long
-    a.ws_rows = cut ? (int32_t)((int64_t)a.r.n_rows * 4 / (3 * (int64_t)a.chunk)) + 1 : 0;
-    const size_t counts = a.r.n_streams > 64 ? 2 * (a.r.n_streams + 1) * sizeof(int32_t) : 0;
-    const size_t lds = S::LDS > counts ? S::LDS : counts;
-    if (cut) {
-        const rh_status st = seq_scratch(ctx);
-        if (st != RH_OK) { *failed = st; return hipSuccess; }
-        a.ws = (float*)ctx->seq_ws;
-        a.blocks = seq_make_div((uint32_t)blocks);
-        a.group_blocks = seq_make_div((uint32_t)group_blocks);
-        hipLaunchKernelGGL((k_seq_scan<T, LN, K, FULL, false>), dim3((unsigned)(((int64_t)a.r.n_rows / a.chunk + 1) * blocks)), dim3(256), lds, ctx->stream, a);
-        hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
-        a.blocks = seq_make_div((uint32_t)wide);
-        const int64_t most = (int64_t)a.r.n_rows * 2 / (3 * (int64_t)a.chunk) + 1;       // streams that are cut
-        hipLaunchKernelGGL((k_seq_scan_carry<LN, S::ROWS, FULL>), dim3((unsigned)((most < a.r.n_streams ? most : a.r.n_streams) * wide)), dim3(256), counts, ctx->stream, a);
-        e = hipGetLastError();
-        if (e != hipSuccess) return e;
-    }
     a.blocks = seq_make_div((uint32_t)blocks);
     a.group_blocks = seq_make_div((uint32_t)group_blocks);
-    hipLaunchKernelGGL((k_seq_scan<T, LN, K, FULL, true>), dim3((unsigned)(((int64_t)a.r.n_rows / a.chunk + a.r.n_streams) * blocks)), dim3(256), lds, ctx->stream, a);
+    // Rows a chunk: enough workgroups for the GPU where streams are few, and no more states than the scratch memory holds.  Nothing is cut where the channels alone are enough:
+    // so (4/3 rows / chunk + 1) * blocks, the counters that there may be, stay below (8/3 + 4) a CU of the 16.
+    const int64_t room = SCAN_ROOM(ctx) / ((int64_t)a.channels * (S::N + 1));
+    const int64_t least = room > 0 ? (int64_t)a.r.n_rows * 4 / (3 * room) + 1 : SCAN_WHOLE;
+    int64_t chunk = (int64_t)a.r.n_rows * blocks / (SCAN_TARGET * ctx->n_cu);
+    chunk = chunk < SCAN_LEAST ? SCAN_LEAST : chunk;
+    chunk = chunk < least ? least : chunk;
+    a.chunk = (int32_t)(chunk > SCAN_WHOLE || blocks > 4 * ctx->n_cu ? SCAN_WHOLE : chunk);
+    const bool cut = 2 * (int64_t)a.r.n_rows >= 3 * (int64_t)a.chunk;        // otherwise no stream can be as long
+    a.ws_rows = cut ? (int32_t)((int64_t)a.r.n_rows * 4 / (3 * (int64_t)a.chunk)) + 1 : 0;
+    const size_t counts = a.r.n_streams > 64 ? (2 * (a.r.n_streams + 1) + STREAMS_T / 64) * sizeof(int32_t) : 0, stage = S::LDS + (FULL ? 0 : 2 * sizeof(int32_t));
+    const size_t lds = stage > counts ? stage : counts;
+    if (cut) {
+        rh_status st = seq_counters(ctx);
+        if (st == RH_OK) st = seq_scratch(ctx);
+        if (st != RH_OK) { *failed = st; return hipSuccess; }
+        a.ws = (float*)ctx->seq_ws; a.count = ctx->seq_cnt;
+    }
+    // as many workgroups as any offsets give
+    if (cut) {
+        hipLaunchKernelGGL((k_seq_scan<T, WL, NS, FULL, false>), dim3((unsigned)(((int64_t)a.r.n_rows / a.chunk + 1) * blocks)), dim3(256), lds, ctx->stream, a);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL((k_seq_scan<T, WL, NS, FULL, true>), dim3((unsigned)(((int64_t)a.r.n_rows / a.chunk + a.r.n_streams) * blocks)), dim3(256), lds, ctx->stream, a);
     return hipGetLastError();
 }
 
