@@ -79,6 +79,7 @@ __device__ __forceinline__ float seq_sum(float v)            // of the wave, the
 template <typename V> struct __attribute__((packed, aligned(1))) seq_loose { V v; };
 template <typename V> __device__ __forceinline__ V seq_load(const void* p) { return ((const seq_loose<V>*)p)->v; }
 template <typename V> __device__ __forceinline__ void seq_store(void* p, V v) { ((seq_loose<V>*)p)->v = v; }
+template <typename V> __device__ __forceinline__ void seq_store_past(void* p, V v) { __builtin_nontemporal_store(v, &((seq_loose<V>*)p)->v); }       // past the L2
 
 __device__ __forceinline__ float seq_to_f32(float v) { return v; }
 __device__ __forceinline__ float seq_to_f32(__bf16 v) { return (float)v; }

@@ -1,13 +1,14 @@
 // rh_state_conv: short causal convolution along the tokens of every stream, a channel at a time.
 //
-// Bound by memory: every input is read once and every output written once; the width - 1 inputs ahead of a thread's rows are read again, by default out of an L2.
+// Bound by memory: every input is read once and every output written once (past the L2: 58 -> 52 us below); the width - 1 inputs ahead of a thread's rows are read again (30 streams of
+// 920 rows, 2048 channels in bf16, inputs that no cache holds: 227 MB and 23 read twice in 51 us, 4.4 TB/s).
 // A thread has 16 bytes of channels and a run of rows, whose last inputs it keeps in registers.  Runs begin where streams do,
 // so that only a stream's first run looks at its state, and that thread, once it has read it, writes the state behind the last row:
 // no other thread reads or writes it, and it may be replaced in place.
 #include "seq_rows.h"
 #include "seq_streams.h"
 
-#define CONV_BATCH 8             // rows whose loads are in flight together
+#define CONV_BATCH 4             // rows whose loads are in flight together, while the four ahead are worked on (eight: 57 for 51 us, see below)
 
 struct conv_args {
     streams_args r;
@@ -16,7 +17,8 @@ struct conv_args {
     void *state, *y;
     int64_t x_stride, y_stride;
     seq_div pieces;              // threads a row
-    int32_t channels, silu, run;
+    int32_t channels, silu, run, log_run;
+    bool past;
 };
 
 template <typename T, int W>
@@ -86,21 +88,37 @@ template <typename T, int W>
 __global__ __launch_bounds__(STREAMS_T) void k_seq_conv(conv_args a)
 {
     constexpr int E = 16 / sizeof(T);
-    extern __shared__ int32_t s_first[];                     // runs of the streams before
+    extern __shared__ int32_t s_first[];                     // of more than 64 streams: runs of the streams before
     __shared__ int32_t s_wave[STREAMS_T / 64];
-    streams_sums(a.r, s_first, s_wave, [&](int32_t n) { return (n + a.run - 1) / a.run; });
     const uint32_t id = blockIdx.x * STREAMS_T + threadIdx.x;
     const int q = (int)seq_quot(id, a.pieces), c = (int)(id - (uint32_t)q * a.pieces.d) * E;
-    if (q >= s_first[a.r.n_streams]) return;
-    const int b = streams_find(s_first, a.r.n_streams, q);
-    int32_t begin, end;
-    streams_rows(a.r, b, begin, end);
-    const int64_t first = begin + (int64_t)(q - s_first[b]) * a.run;
+    conv_taps<T, W> taps;
+    taps.load(a, c);                                         // on their way while the run is looked for
+    auto runs = [&](int32_t n) { return (int32_t)(((uint32_t)n + a.run - 1) >> a.log_run); };
+    int32_t begin, end, all;
+    int64_t first;
+    int b;
+    if (a.r.n_streams <= 64) {
+        const streams_lane s = streams_few(a.r, runs, all);
+        b = 0;
+#pragma unroll
+        for (int step = 32; step; step >>= 1) {
+            const int32_t ahead = __shfl(s.before, b + step);               // every lane of the wave takes part
+            if (b + step < a.r.n_streams && ahead <= q) b += step;
+        }
+        begin = __shfl(s.begin, b); end = __shfl(s.end, b);
+        first = begin + (int64_t)(q - __shfl(s.before, b)) * a.run;
+        if (q >= all) return;
+    } else {
+        streams_sums(a.r, s_first, s_wave, runs);
+        if (q >= s_first[a.r.n_streams]) return;
+        b = streams_find(s_first, a.r.n_streams, q);
+        streams_rows(a.r, b, begin, end);
+        first = begin + (int64_t)(q - s_first[b]) * a.run;
+    }
     if (first < begin || first >= end) return;               // offsets that do not ascend
     const int32_t row = (int32_t)first, stop = end - row < a.run ? end : row + a.run;
     const T* x = (const T*)a.x;
-    conv_taps<T, W> taps;
-    taps.load(a, c);
 
     float v[W - 1 + CONV_BATCH][E];
     if (row > begin) {                                       // a run is W - 1 rows or more: they are all the stream's
@@ -132,17 +150,28 @@ __global__ __launch_bounds__(STREAMS_T) void k_seq_conv(conv_args a)
             }
         }
     }
-    for (int32_t t = row; t < stop; t += CONV_BATCH) {
-        u32x4 in[CONV_BATCH];
+    const T* px = x + (int64_t)row * a.x_stride;
+    T* py = (T*)a.y + (int64_t)row * a.y_stride + c;
+    const bool whole = a.channels - c >= E;
+    u32x4 in[CONV_BATCH];
+    auto load = [&](int rows) __attribute__((always_inline)) {               // rows that are left
 #pragma unroll
-        for (int i = 0; i < CONV_BATCH; ++i) in[i] = row_load<T, E>(x + (int64_t)(t + i < stop ? t + i : stop - 1) * a.x_stride, c, a.channels);
+        for (int i = 0; i < CONV_BATCH; ++i) in[i] = row_load<T, E>(px + (i < rows ? i : rows - 1) * a.x_stride, c, a.channels);
+        px += CONV_BATCH * a.x_stride;
+    };
+    load(stop - row);
+    for (int32_t t = row; t < stop; t += CONV_BATCH) {
+        const int rows = stop - t;
+#pragma unroll
+        for (int i = 0; i < CONV_BATCH; ++i) row_place<T, E>(in[i], c, a.channels, v[W - 1 + i]);
+        if (rows > CONV_BATCH) load(rows - CONV_BATCH);      // while these are worked on
 #pragma unroll
         for (int i = 0; i < CONV_BATCH; ++i) {
             float y[E];
-            row_place<T, E>(in[i], c, a.channels, v[W - 1 + i]);
             taps.apply(v, i, a.silu, y);
-            if (t + i < stop) row_store<T, E>((T*)a.y + (int64_t)(t + i) * a.y_stride + c, a.channels - c, y);
+            if (i < rows) row_store<T, E>(py + i * a.y_stride, whole ? E : a.channels - c, y, a.past);
         }
+        py += CONV_BATCH * a.y_stride;
 #pragma unroll
         for (int j = 0; j < W - 1; ++j)
 #pragma unroll
@@ -159,7 +188,7 @@ static void launch_conv(rh_ctx* ctx, conv_args& a)
         return;
     }
     const int64_t threads = ((int64_t)a.r.n_rows / a.run + a.r.n_streams) * a.pieces.d;       // as many runs as any offsets give
-    hipLaunchKernelGGL((k_seq_conv<T, W>), dim3((unsigned)((threads + STREAMS_T - 1) / STREAMS_T)), dim3(STREAMS_T), (a.r.n_streams + 1) * sizeof(int32_t), ctx->stream, a);
+    hipLaunchKernelGGL((k_seq_conv<T, W>), dim3((unsigned)((threads + STREAMS_T - 1) / STREAMS_T)), dim3(STREAMS_T), a.r.n_streams > 64 ? (a.r.n_streams + 1) * sizeof(int32_t) : 0, ctx->stream, a);
 }
 template <typename T>
 static void launch_conv(rh_ctx* ctx, conv_args& a, int width)
@@ -202,13 +231,15 @@ extern "C" rh_status rh_state_conv(rh_ctx* ctx, const rh_state_rows* rows, const
     if (rows->n_rows == 0 || rows->n_streams == 0) return RH_OK;
     if (!x || !y || (rows->n_slots && !state)) RH_FAIL(ctx, RH_E_INVALID, "rh_state_conv: null argument");
     const int E = type == RH_T_F32 ? 4 : 8, pieces = (channels + E - 1) / E;
-    // Longer runs read less twice; shorter ones where there would be too few to fill the GPU.
-    a.run = 32;
-    while (a.run > CONV_BATCH && (int64_t)rows->n_rows / a.run * pieces < (int64_t)ctx->n_cu * 4 * STREAMS_T) a.run /= 2;
-    if (((int64_t)rows->n_rows / (rows->offsets ? a.run : 1) + rows->n_streams) * pieces > 0x7FFFFF00ll)
+    // Rows a run: 16, and 8 where that would be fewer than two workgroups a CU.  8, 16, 32 and 64 of them, us, inputs that no cache holds: 30 streams of 920, 2048 channels in bf16 54, 51,
+    // 59 and 53 (32 leave three workgroups and a half a CU); 37 of up to 1500, 515 in fp32 29.3, 26.4, 29.1 and 40.5.
+    a.log_run = ((int64_t)rows->n_rows >> 4) * pieces < (int64_t)ctx->n_cu * 2 * STREAMS_T ? 3 : 4;
+    a.run = 1 << a.log_run;
+    if (((int64_t)rows->n_rows / (rows->offsets ? a.run : 1) + rows->n_streams) * pieces > 0x7FFFF000ll)
         RH_FAIL(ctx, RH_E_SHAPE, "rh_state_conv: %d rows of %d channels", rows->n_rows, channels);
     a.x = x; a.weight = weight; a.bias = bias; a.state = state; a.y = y; a.x_stride = x_stride; a.y_stride = y_stride;
     a.pieces = seq_make_div((uint32_t)pieces); a.channels = channels; a.silu = silu != 0;
+    a.past = (int64_t)rows->n_rows * channels * (type == RH_T_F32 ? 4 : 2) >= ROWS_PAST;
     if (type == RH_T_F32) launch_conv<float>(ctx, a, width); else launch_conv<__bf16>(ctx, a, width);
     RH_HIP(ctx, hipGetLastError());
     return RH_OK;

@@ -47,12 +47,15 @@ __device__ __forceinline__ void row_put(uint8_t* p, int bytes, u32x4 w)
     if (B < 2 && (bytes & 1)) *p = (uint8_t)w[0];
 }
 
+// past: whole pieces past the L2, for what the kernel does not read again and the L2s do not hold anyway
 template <typename T, int E>
-__device__ __forceinline__ void row_store(T* p, int n, const float (&v)[E])
+__device__ __forceinline__ void row_store(T* p, int n, const float (&v)[E], bool past = false)
 {
     u32x4 w;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
         if constexpr (sizeof(T) == 2) w[i] = seq_pack_bf16(v[2 * i], v[2 * i + 1]); else w[i] = __float_as_uint(v[i]);
-    row_put<(int)sizeof(T)>((uint8_t*)p, n * (int)sizeof(T), w);
+    if (past && n >= E) seq_store_past(p, w);
+    else row_put<(int)sizeof(T)>((uint8_t*)p, n * (int)sizeof(T), w);
 }
+#define ROWS_PAST (32ll << 20)   // bytes of output from which on: as many as the eight L2s have

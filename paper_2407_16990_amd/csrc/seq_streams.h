@@ -59,6 +59,19 @@ __device__ __forceinline__ void streams_sums(const streams_args& r, int32_t* s, 
     if (t == STREAMS_T - 1) s[r.n_streams] = before;         // it has the last streams, or none behind them
     __syncthreads();
 }
+// The same of up to 64 streams, a stream a lane: its rows, and the sum over the streams before it.
+struct streams_lane { int32_t begin, end, before; };
+template <typename F>
+__device__ __forceinline__ streams_lane streams_few(const streams_args& r, F count, int32_t& all)
+{
+    const int lane = threadIdx.x & 63;
+    streams_lane s = {0, 0, 0};
+    if (lane < r.n_streams) streams_rows(r, lane, s.begin, s.end);
+    const int32_t n = count(s.end - s.begin), upto = seq_scan(n);
+    all = __builtin_amdgcn_readlane(upto, 63);
+    s.before = upto - n;
+    return s;
+}
 // Largest b in [0, n) with s[b] <= q; s ascending, s[0] = 0 <= q.
 __device__ __forceinline__ int streams_find(const int32_t* s, int n, int32_t q)
 {
