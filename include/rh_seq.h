@@ -130,7 +130,7 @@ rh_status rh_matvec_packed(rh_ctx* ctx, const void* x, int32_t x_type, int64_t x
 /*
  * The rows (tokens) of a call and where their streams' states lie in a pool of n_slots, all in device memory.
  *   offsets i32 [n_streams + 1], ascending: rows [offsets[b], offsets[b+1]) are the new tokens of stream b, in order; rows of no stream are left as they are.
- *     NULL: one row a stream (n_rows = n_streams).  Offsets outside [0, n_rows] count as its ends.
+ *     NULL: one row a stream (n_rows = n_streams).  Offsets outside [0, n_rows] count as its ends; where any descend, the call writes nothing.
  *   slots i32 [n_streams]: the stream's state before the call; into i32 [n_streams] (NULL: slots): where its state afterwards goes, so
  *     that the one before may stay.  A slot outside [0, n_slots): a state of zeros; an `into` outside: not kept.
  *   past i32 [n_streams] (NULL: all have one): 0 or below where a stream begins with this call: its state before is zeros, whatever its slot holds.
@@ -138,7 +138,7 @@ rh_status rh_matvec_packed(rh_ctx* ctx, const void* x, int32_t x_type, int64_t x
  */
 typedef struct {
     const int32_t *offsets, *slots, *into, *past;
-    int32_t n_streams, n_rows, n_slots;                /* n_streams at most RH_SEQ_MAX_STREAMS where there are offsets */
+    int32_t n_streams, n_rows, n_slots;                /* n_streams at most RH_SEQ_MAX_STREAMS where there are offsets; n_rows at most 2^31 - 2^16 */
 } rh_state_rows;
 
 /*

@@ -316,16 +316,23 @@ static const at::Tensor& as(const context& on, PyObject* o, const at::Tensor& li
     return t;
 }
 static int64_t row_stride(const at::Tensor& t) { return t.size(0) > 1 ? t.stride(0) : t.size(1); }
-// no element of one matrix lies in the other: all of it ahead or behind, or columns side by side in rows of one length
-static bool apart(const at::Tensor& a, const at::Tensor& b)
+// no element of one matrix (its rows' elements side by side) lies in the other: all of it ahead or behind, or columns side by side in rows of one length
+struct matrix {
+    int64_t at, rows, stride, bytes;                         // bytes: of a row's elements
+    explicit matrix(const at::Tensor& t)
+    {
+        const int64_t size = (int64_t)t.element_size();
+        at = (int64_t)t.data_ptr(); rows = t.size(0);
+        bytes = rows ? t.numel() / rows * size : 0;
+        stride = rows > 1 ? t.stride(0) * size : bytes;
+    }
+};
+static bool apart(const matrix& a, const matrix& b)
 {
-    if (!a.numel() || !b.numel()) return true;
-    const int64_t size = (int64_t)a.element_size(), wide = row_stride(a) * size, p = (int64_t)a.data_ptr(), q = (int64_t)b.data_ptr();
-    auto bytes = [&](const at::Tensor& t) { return ((t.size(0) - 1) * row_stride(t) + t.size(1)) * size; };
-    if (p + bytes(a) <= q || q + bytes(b) <= p) return true;
-    if (row_stride(a) != row_stride(b) || a.size(0) < 2) return false;
-    const int64_t at = ((q - p) % wide + wide) % wide;       // b's columns in a's rows
-    return at >= a.size(1) * size && at + b.size(1) * size <= wide;
+    if (!a.bytes || !b.bytes || a.at + (a.rows - 1) * a.stride + a.bytes <= b.at || b.at + (b.rows - 1) * b.stride + b.bytes <= a.at) return true;
+    if (a.rows < 2 || b.rows < 2 || a.stride != b.stride || a.stride <= 0) return false;
+    const int64_t at = ((b.at - a.at) % a.stride + a.stride) % a.stride;     // b's columns in a's rows
+    return at >= a.bytes && at + b.bytes <= a.stride;
 }
 
 // state_conv(ctx, x, weight, state, slots, bias, offsets, past, into, silu, out) -> out
@@ -349,7 +356,7 @@ static PyObject* state_conv(PyObject*, PyObject* const* a, Py_ssize_t nargs)
     const rh_state_rows rows = rows_of(on, a[6], a[4], a[7], a[8], x.size(0), state.size(0));
     const bool silu = truth(a[9], "silu");
     const at::Tensor out = given(a[10]) ? as(on, a[10], x, "out as x") : fresh(x.sizes(), x, x.scalar_type());
-    need(!given(a[10]) || apart(out, x), "out apart from x");
+    need(!given(a[10]) || (apart(matrix(out), matrix(x)) && apart(matrix(out), matrix(state))), "out apart from x and state");
     const rh_status st = f_conv(on.handle, &rows, x.data_ptr(), row_stride(x), (const float*)weight.data_ptr(), bias, type_of(x), channels, width, silu, state.data_ptr(),
                                 out.data_ptr(), row_stride(out));
     if (st != RH_OK) return status(st);
@@ -392,7 +399,11 @@ static PyObject* state_scan(PyObject*, PyObject* const* a, Py_ssize_t nargs)
     in.softplus = truth(a[11], "softplus");
     const rh_state_rows rows = rows_of(on, a[12], a[7], a[13], a[14], x.size(0), state.size(0));
     const at::Tensor out = given(a[15]) ? as(on, a[15], x, "out as x") : fresh(x.sizes(), x, x.scalar_type());
-    need(!given(a[15]) || (apart(out, x) && apart(out, dt) && (!gate || apart(out, *gate))), "out apart from x, dt and gate");
+    if (given(a[15])) {
+        const matrix y(out);
+        need(apart(y, matrix(x)) && apart(y, matrix(dt)) && (!gate || apart(y, matrix(*gate))) && apart(y, matrix(b)) && apart(y, matrix(c)) && apart(y, matrix(state)),
+             "out apart from the inputs and the state");
+    }
     const rh_status st = f_scan(on.handle, &rows, &in, (float*)state.data_ptr(), out.data_ptr(), row_stride(out));
     if (st != RH_OK) return status(st);
     return wrap(out);

@@ -96,10 +96,11 @@ __global__ __launch_bounds__(STREAMS_T) void k_seq_conv(conv_args a)
     taps.load(a, c);                                         // on their way while the run is looked for
     auto runs = [&](int32_t n) { return (int32_t)(((uint32_t)n + a.run - 1) >> a.log_run); };
     int32_t begin, end, all;
-    int64_t first;
+    int32_t row;
     int b;
     if (a.r.n_streams <= 64) {
-        const streams_lane s = streams_few(a.r, runs, all);
+        streams_lane s;
+        if (!streams_few(a.r, runs, s, all)) return;
         b = 0;
 #pragma unroll
         for (int step = 32; step; step >>= 1) {
@@ -107,17 +108,15 @@ __global__ __launch_bounds__(STREAMS_T) void k_seq_conv(conv_args a)
             if (b + step < a.r.n_streams && ahead <= q) b += step;
         }
         begin = __shfl(s.begin, b); end = __shfl(s.end, b);
-        first = begin + (int64_t)(q - __shfl(s.before, b)) * a.run;
+        row = begin + (q - __shfl(s.before, b)) * a.run;
         if (q >= all) return;
     } else {
-        streams_sums(a.r, s_first, s_wave, runs);
-        if (q >= s_first[a.r.n_streams]) return;
+        if (!streams_sums(a.r, s_first, s_wave, runs) || q >= s_first[a.r.n_streams]) return;
         b = streams_find(s_first, a.r.n_streams, q);
         streams_rows(a.r, b, begin, end);
-        first = begin + (int64_t)(q - s_first[b]) * a.run;
+        row = begin + (q - s_first[b]) * a.run;
     }
-    if (first < begin || first >= end) return;               // offsets that do not ascend
-    const int32_t row = (int32_t)first, stop = end - row < a.run ? end : row + a.run;
+    const int32_t stop = end - row < a.run ? end : row + a.run;
     const T* x = (const T*)a.x;
 
     float v[W - 1 + CONV_BATCH][E];
@@ -206,7 +205,7 @@ static void launch_conv(rh_ctx* ctx, conv_args& a, int width)
 
 rh_status streams_check(rh_ctx* ctx, const char* name, const rh_state_rows* r, streams_args* a)
 {
-    if (r->n_streams < 0 || r->n_rows < 0 || r->n_slots < 0) RH_FAIL(ctx, RH_E_SHAPE, "%s: %d rows of %d streams, %d slots", name, r->n_rows, r->n_streams, r->n_slots);
+    if (r->n_streams < 0 || r->n_rows < 0 || r->n_slots < 0 || r->n_rows > 0x7FFF0000) RH_FAIL(ctx, RH_E_SHAPE, "%s: %d rows of %d streams, %d slots", name, r->n_rows, r->n_streams, r->n_slots);
     if (r->n_streams && !r->slots) RH_FAIL(ctx, RH_E_INVALID, "%s: null argument", name);
     if (!r->offsets && r->n_rows != r->n_streams) RH_FAIL(ctx, RH_E_SHAPE, "%s: %d rows of %d streams without offsets", name, r->n_rows, r->n_streams);
     if (r->offsets && r->n_streams > RH_SEQ_MAX_STREAMS)

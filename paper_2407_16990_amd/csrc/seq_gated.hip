@@ -141,7 +141,7 @@ __global__ __launch_bounds__(GATED_MAX_T) void k_seq_gated(gated_args a)
 }
 
 template <typename T>
-static void launch_gated(hipStream_t s, gated_args& a)
+static bool launch_gated(hipStream_t s, gated_args& a)       // false: more workgroups than a launch takes
 {
     constexpr int E = 16 / sizeof(T);
     const int pieces = (a.per + E - 1) / E;
@@ -156,7 +156,9 @@ static void launch_gated(hipStream_t s, gated_args& a)
     if (rounds > 1) threads = GATED_MAX_T;
     else while (threads < wide) threads *= 2;
     a.rows_wg = rounds > 1 ? 1 : (int)(threads / wide);
-    const dim3 grid((unsigned)((a.rows + a.rows_wg - 1) / a.rows_wg));
+    const int64_t wgs = ((int64_t)a.rows + a.rows_wg - 1) / a.rows_wg;
+    if (wgs * threads > 0xFFFFFFFFll) return false;
+    const dim3 grid((unsigned)wgs);
 #define N(ITEMS, ROUNDS) hipLaunchKernelGGL((k_seq_gated<T, ITEMS, ROUNDS>), grid, dim3(threads), 0, s, a)
     // a row has 4096 pieces (bf16) or 8192 (fp32) at most, and more than half of a group's places for them are taken
     if (rounds == 1) { if (items == 1) N(1, 1); else if (items == 2) N(2, 1); else if (items == 4) N(4, 1); else if constexpr (E == 4) N(8, 1); }
@@ -165,6 +167,7 @@ static void launch_gated(hipStream_t s, gated_args& a)
     else if (rounds == 8) { if (items == 1) N(1, 8); else if constexpr (E == 4) N(2, 8); }
     else if constexpr (E == 4) N(1, 16);
 #undef N
+    return true;
 }
 
 extern "C" rh_status rh_norm_gated(rh_ctx* ctx, const void* x, int64_t x_stride, const void* gate, int64_t gate_stride, const float* weight,
@@ -187,7 +190,8 @@ extern "C" rh_status rh_norm_gated(rh_ctx* ctx, const void* x, int64_t x_stride,
     a.x = x; a.gate = gate; a.weight = weight; a.y = y; a.y8 = y8; a.y8_scale = y8_scale; a.x_stride = x_stride; a.gate_stride = gate_stride;
     a.groups = seq_make_div((uint32_t)groups); a.rows = n_rows; a.cols = n_cols; a.per = n_cols / groups; a.eps = eps;
     a.past = (int64_t)n_rows * n_cols * (type == RH_T_F32 ? 4 : 2) >= ROWS_PAST;
-    if (type == RH_T_F32) launch_gated<float>(ctx->stream, a); else launch_gated<__bf16>(ctx->stream, a);
+    if (!(type == RH_T_F32 ? launch_gated<float>(ctx->stream, a) : launch_gated<__bf16>(ctx->stream, a)))
+        RH_FAIL(ctx, RH_E_SHAPE, "rh_norm_gated: %d rows of %d elements", n_rows, n_cols);
     RH_HIP(ctx, hipGetLastError());
     return RH_OK;
 }

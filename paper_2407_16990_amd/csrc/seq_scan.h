@@ -174,25 +174,22 @@ __device__ __forceinline__ bool scan_find(const scan_args& a, int32_t q, int32_t
     auto own = [&](int32_t len) { const scan_cut<ROWS> k(len, a.chunk); return OUT ? k.n : k.n < 2 ? 0 : k.n - 1; };
     auto rows = [&](int32_t len) { const scan_cut<ROWS> k(len, a.chunk); return k.n < 2 ? 0 : k.n; };
     if (a.r.n_streams <= 64) {                               // a stream a lane
-        const int lane = threadIdx.x & 63;
-        int32_t begin = 0, end = 0;
-        if (lane < a.r.n_streams) streams_rows(a.r, lane, begin, end);
-        const int32_t mine = own(end - begin), wide = rows(end - begin), upto = seq_scan(mine), ahead = seq_scan(wide) - wide;
-        const uint64_t hit = __ballot(q >= upto - mine && q < upto);
-        if (!hit) return false;
-        b = __builtin_ctzll(hit);
-        place = q - __builtin_amdgcn_readlane(upto - mine, b);
-        row = __builtin_amdgcn_readlane(ahead, b);
+        streams_lane s, wide;
+        int32_t all, unused;
+        if (!streams_few(a.r, own, s, all) || q >= all) return false;
+        streams_few(a.r, rows, wide, unused);
+        b = __builtin_ctzll(__ballot(q >= s.before && q < s.before + s.count));
+        place = q - __builtin_amdgcn_readlane(s.before, b);
+        row = __builtin_amdgcn_readlane(wide.before, b);
     } else {
         int32_t *s_rows = s_mem + a.r.n_streams + 1, *s_wave = s_rows + a.r.n_streams + 1;
-        streams_sums(a.r, s_mem, s_wave, own);
+        if (!streams_sums(a.r, s_mem, s_wave, own) || q >= s_mem[a.r.n_streams]) return false;
         streams_sums(a.r, s_rows, s_wave, rows);
-        if (q >= s_mem[a.r.n_streams]) return false;
         b = __builtin_amdgcn_readfirstlane(streams_find(s_mem, a.r.n_streams, q));
         place = q - __builtin_amdgcn_readfirstlane(s_mem[b]);
         row = __builtin_amdgcn_readfirstlane(s_rows[b]);
     }
-    return place >= 0;
+    return true;
 }
 
 #define SCAN_AHEAD 8             // chunks whose states and sums are in flight
@@ -255,10 +252,10 @@ __device__ __forceinline__ void scan_chunk(const scan_args& a, f32x4* s_stage, i
         skip[e] = OUT && a.skip && e < left ? a.skip[cg + e] : 0.f;
     }
     // where its first piece of a stage's rows lies, and its first quad
-    const T *px = (const T*)a.x + (int64_t)(first + pr) * a.x_stride + cc, *pd = (const T*)a.dt + (int64_t)(first + pr) * a.dt_stride + cc;
-    const T *pz = (const T*)a.gate + (int64_t)(first + pr) * a.gate_stride + cc;
-    const T *pb = (const T*)a.b + (int64_t)(first + br) * a.b_stride + (int64_t)g * a.n, *pq = (const T*)a.c + (int64_t)(first + br) * a.c_stride + (int64_t)g * a.n;
-    T* py = (T*)a.y + (int64_t)(first + pr) * a.y_stride + cg;
+    const T *px = (const T*)a.x + ((int64_t)first + pr) * a.x_stride + cc, *pd = (const T*)a.dt + ((int64_t)first + pr) * a.dt_stride + cc;
+    const T *pz = (const T*)a.gate + ((int64_t)first + pr) * a.gate_stride + cc;
+    const T *pb = (const T*)a.b + ((int64_t)first + br) * a.b_stride + (int64_t)g * a.n, *pq = (const T*)a.c + ((int64_t)first + br) * a.c_stride + (int64_t)g * a.n;
+    T* py = (T*)a.y + ((int64_t)first + pr) * a.y_stride + cg;
     struct raw { u32x4 x[NX], dt[NX]; f32x4 b[NB], c[NB]; };
     u32x4 gate[NX];
     auto piece = [&](const T* p) __attribute__((always_inline)) { return narrow ? row_load<T, E>(p, cg, c_end) : seq_load<u32x4>(p); };
@@ -467,7 +464,12 @@ __device__ __forceinline__ void scan_chunk(const scan_args& a, f32x4* s_stage, i
                     *(f32x4*)state_at(c0 + i, q) = v;
                     const f32x4 more = __builtin_bit_cast(f32x4, add[i]);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] = fmaf(__builtin_amdgcn_exp2f(__uint_as_float(sum[i]) * fade[q][e]), v[e], more[e]);
+                    for (int e = 0; e < 4; ++e) {
+                        // what fades to nothing over a chunk, step by step was more each time: an infinite state stays infinite
+                        const float f = __builtin_amdgcn_exp2f(__uint_as_float(sum[i]) * fade[q][e]);
+                        v[e] = fmaf(f == 0.f ? 0x1p-149f : f, v[e], more[e]);
+                        if (!FULL && n0 + 4 * q + e >= a.n) v[e] = 0.f;                  // a state that is none: an infinite sum times its zero
+                    }
                 }
             }
         }
@@ -485,7 +487,6 @@ __global__ __launch_bounds__(256, 2) void k_seq_scan(scan_args a)
     if (!scan_find<ROWS, OUT>(a, (int32_t)item, (int32_t*)s_stage, b, place, ws_row)) return;
     streams_rows(a.r, b, begin, end);
     const scan_cut<ROWS> cut(end - begin, a.chunk);
-    if (place >= cut.n || (cut.n > 1 && ws_row + cut.n > a.ws_rows)) return;             // offsets that do not ascend
     const int32_t first = begin + place * cut.size, stop = end - first < cut.size ? end : first + cut.size;
     scan_chunk<T, LN, NS, FULL, OUT>(a, s_stage, b, place, ws_row, cut.n, (int32_t)blk, first, stop);
 }
@@ -508,7 +509,7 @@ static hipError_t launch_scan(rh_ctx* ctx, scan_args& a, rh_status* failed)
     a.blocks = seq_make_div((uint32_t)blocks);
     a.group_blocks = seq_make_div((uint32_t)group_blocks);
     // Rows a chunk: enough workgroups for the GPU where streams are few, and no more states than the scratch memory holds.  Nothing is cut where the channels alone are enough:
-    // so (4/3 rows / chunk + 1) * blocks, the counters that there may be, stay below (8/3 + 4) a CU of the 16.
+    // so (4/3 rows / chunk + 1) * blocks, the counters that there may be, stay below 5.4 + 4 a CU of the 16.
     const int64_t room = SCAN_ROOM(ctx) / ((int64_t)a.channels * (S::N + 1));
     const int64_t least = room > 0 ? (int64_t)a.r.n_rows * 4 / (3 * room) + 1 : SCAN_WHOLE;
     int64_t chunk = (int64_t)a.r.n_rows * blocks / (SCAN_TARGET * ctx->n_cu);

@@ -340,6 +340,24 @@ def test_scan_infinities_are_what_the_formula_makes_of_them(rh, dtype, n):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n", [5, 13, 16, 100])
+def test_scan_infinities_reach_the_chunks_behind(rh, dtype, n):
+    """In a stream that is cut, also where a chunk fades to nothing: the state and every later row are infinite, as step by step; other channels stay finite."""
+    channels, rows, at = 9, 1500, 40
+    s = Streams(np.random.default_rng(0), [rows])
+    i = _scan_inputs(_gen(9), s, channels, n, 1, dtype, gate=False, skip=False, steps=(0.05, 2.0), spread=0.1)
+    i = {k: v if v is None else v.clone() for k, v in i.items()}
+    i["b"], i["c"] = i["b"].abs() + 0.1, i["c"].abs() + 0.1
+    i["x"][at, 3] = float("inf")
+    state = i.pop("state")
+    y = rh.state_scan(**i, state=state, slots=s.slots, **s.kw()).float()
+    assert bool(torch.isposinf(y[at:, 3]).all()) and bool(torch.isfinite(y[:at, 3]).all())
+    assert bool(torch.isfinite(y[:, [c for c in range(channels) if c != 3]]).all())
+    kept = state[int(s.into[0])]
+    assert bool(torch.isposinf(kept[3]).all()) and int((~torch.isfinite(kept)).sum()) == n
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 def test_scan_row_by_row_is_the_same(rh, dtype):
     """Rows in one call, in calls of pieces and of a row each: within the bounds of each other."""
     rows, channels, n = 90, 70, 16
@@ -440,28 +458,39 @@ def test_offsets_past_32_bits(rh):
 
 
 @pytest.mark.parametrize("n_streams", [3, 100])
-def test_offsets_that_are_none(rh, n_streams):
-    """Offsets that lie outside the rows count as their ends; streams whose offsets descend have no rows; nothing beside the rows is touched."""
-    g, channels, rows = _gen(0), 24, 500
+def test_offsets_that_descend(n_streams):
+    """They write nothing, not the counters between workgroups either: a stream that is cut in a call after them comes out right.  Offsets beyond the rows count as their ends."""
+    rh, fresh = _context(), _context()
+    g, channels, rows = _gen(0), 24, 2000
     guard = torch.full((rows + 20, channels), 5.0, device="cuda")
     out = guard[10:10 + rows]
-    x, w, state = _randn(g, rows, channels), _randn(g, 4, channels), torch.zeros((n_streams, 3, channels), device="cuda")
+    x, w, state = _randn(g, rows, channels), _randn(g, 4, channels), torch.full((n_streams, 3, channels), 3.0, device="cuda")
     s = Streams(np.random.default_rng(0), [rows])
     i = _scan_inputs(g, s, channels, 16, 1, torch.float32)
-    i["state"] = torch.zeros((n_streams, channels, 16), device="cuda")
-    rng = np.random.default_rng(1)
+    i["state"] = torch.full((n_streams, channels, 16), 3.0, device="cuda")
+    rng, slots = np.random.default_rng(1), _i32(np.arange(n_streams))
     for k in range(6):
-        offsets = rng.integers(-2 ** 31, 2 ** 31 - 1, n_streams + 1) if k < 2 else rng.integers(-50, rows + 50, n_streams + 1) if k < 4 else np.full(n_streams + 1, 0)
-        if k == 5:
+        offsets = rng.integers(-2 ** 31, 2 ** 31 - 1, n_streams + 1) if k < 2 else rng.integers(-50, rows + 50, n_streams + 1)
+        if k == 4:
             offsets = np.array([0, rows] * (n_streams // 2 + 1))[:n_streams + 1]         # every other stream has all rows
+        if k == 5:
+            offsets = np.concatenate((np.arange(n_streams), [0]))                        # the last one alone
+        offsets[-2:] = np.clip(offsets[-2:], 1, rows)
+        offsets[-1] = offsets[-2] - 1                                                    # some descend for certain
         print("offsets", k, offsets[:4].tolist(), flush=True)
-        rh.state_conv(x, w, state, _i32(np.arange(n_streams)), offsets=_i32(offsets), out=out)
-        rh.state_scan(**i, slots=_i32(np.arange(n_streams)), offsets=_i32(offsets), out=out)
+        rh.state_conv(x, w, state, slots, offsets=_i32(offsets), out=out)
+        rh.state_scan(**i, slots=slots, offsets=_i32(offsets), out=out)
         torch.cuda.synchronize()
-        assert bool((guard[:10] == 5).all()) and bool((guard[10 + rows:] == 5).all())
-    # the ends: one stream from below the first row to behind the last
-    far = rh.state_conv(x, w, state, _i32([-1]), offsets=_i32([-7, rows + 9]))
-    assert torch.equal(far, rh.state_conv(x, w, state, _i32([-1]), offsets=_i32([0, rows])))
+        assert bool((guard == 5).all()) and bool((state == 3).all()) and bool((i["state"] == 3).all())
+    offsets = np.zeros(n_streams + 1, int)
+    offsets[0], offsets[1:] = -7, rows + 9                                               # the first stream has all, from below the first row to behind the last
+    want = np.zeros(n_streams + 1, int)
+    want[1:] = rows
+    for c in (rh, fresh):
+        c.state_scan(**i, slots=_i32(np.full(n_streams, -1)), offsets=_i32(want))        # the scratch memory is there
+    a = rh.state_scan(**i, slots=_i32(np.full(n_streams, -1)), offsets=_i32(offsets)), rh.state_conv(x, w, state, _i32(np.full(n_streams, -1)), offsets=_i32(offsets))
+    b = fresh.state_scan(**i, slots=_i32(np.full(n_streams, -1)), offsets=_i32(want)), fresh.state_conv(x, w, state, _i32(np.full(n_streams, -1)), offsets=_i32(want))
+    assert all(torch.equal(p, q) for p, q in zip(a, b))
 
 
 def _layer(rh, g, channels, n, dtype):
@@ -625,12 +654,13 @@ def test_tensors_that_do_not_fit_are_refused_in_the_binding(rh):
         lambda: conv(x.cpu(), w, cs, slots), lambda: conv(x.t(), w, cs, slots), lambda: conv(x, w.to(bf), cs, slots), lambda: conv(x, w[:, :7], cs, slots),
         lambda: conv(x, w, cs.to(bf), slots), lambda: conv(x, w, cs[:, :2], slots), lambda: conv(x, w, z(2, 8, 3).transpose(1, 2), slots), lambda: conv(x, w, cs, slots.long()),
         lambda: conv(x, w, cs, slots[:1]), lambda: conv(x, w, cs, slots, bias=z(7)), lambda: conv(x, w, cs, slots, offsets=slots), lambda: conv(x, w, cs, slots, past=slots[:1]),
-        lambda: conv(x, w, cs, slots, into=slots.long()), lambda: conv(x, w, cs, slots, out=out.to(bf)), lambda: conv(x, w, cs, slots, out=out[:1]), lambda: conv(x, w, cs, slots, out=x),
+        lambda: conv(x, w, cs, slots, into=slots.long()), lambda: conv(x, w, cs, slots, out=out.to(bf)), lambda: conv(x, w, cs, slots, out=out[:1]), lambda: conv(x, w, cs, slots, out=x), lambda: conv(x, w, cs, slots, out=cs.view(-1)[16:32].view(2, 8)),
         lambda: conv(row[:, :8], w, cs, slots, out=row[:, 7:15]), lambda: conv([1.0], w, cs, slots),
         lambda: scan(x, x.to(bf), a, b, b, hs, slots), lambda: scan(x, x, a[:7], b, b, hs, slots), lambda: scan(x, x, a, b[:1], b, hs, slots), lambda: scan(x, x, a, b, b[..., :3], hs, slots),
         lambda: scan(x, x, a, b.to(bf), b.to(bf), hs, slots), lambda: scan(x, x, a, b[:, 0], b[:, 0], hs, slots), lambda: scan(x, x, a, b, b, hs.to(bf), slots), lambda: scan(x, x, a, b, b, hs[..., :3], slots),
         lambda: scan(x, x, a, z(2, 4, 1).transpose(1, 2)[..., :4].expand(2, 1, 4)[:, :, ::2], b, hs, slots), lambda: scan(x, x, a, b, b, hs, slots[:1]), lambda: scan(x, x, a, b, b, hs, slots, skip=z(7)),
-        lambda: scan(x, x, a, b, b, hs, slots, gate=x[:1]), lambda: scan(x, x, a, b, b, hs, slots, dt_bias=z(8, dtype=bf)), lambda: scan(x, x, a, b, b, hs, slots, out=x),
+        lambda: scan(x, x, a, b, b, hs, slots, gate=x[:1]), lambda: scan(x, x, a, b, b, hs, slots, dt_bias=z(8, dtype=bf)), lambda: scan(x, x, a, b, b, hs, slots, out=x), lambda: scan(x, x, a, row[:, 4:8].unflatten(1, (1, 4)), b, hs, slots, out=row[:, :8]),
+        lambda: scan(x, x, a, b, row[:, 7:11].unflatten(1, (1, 4)), hs, slots, out=row[:, :8]), lambda: scan(x, x, a, b, b, hs, slots, out=hs.view(-1)[8:24].view(2, 8)),
         lambda: scan(x, z(2, 8), a, b, b, hs, slots, gate=row[:, :8], out=row[:, 4:12]), lambda: scan(x, x, a, b, b, hs, slots, offsets=_i32([0, 1])),
         lambda: rh.norm_gated(x, x[:1], z(8)), lambda: rh.norm_gated(x, x.to(bf), z(8)), lambda: rh.norm_gated(x, x, z(7)), lambda: rh.norm_gated(x, x, z(8), outputs="bf16"), lambda: rh.norm_gated(x.t(), x.t(), z(2)),
     ]
@@ -654,6 +684,8 @@ def test_tensors_that_do_not_fit_are_refused_in_the_binding(rh):
     assert bool((out == 5).all())
     # columns of the same rows side by side are apart
     side = rh.state_conv(row[:, :8], w, cs, slots, out=row[:, 8:16])
+    assert side.data_ptr() == row[:, 8:16].data_ptr()
+    side = rh.state_scan(row[:, :8], x, a, row[:, 16:20].unflatten(1, (1, 4)), row[:, 20:].unflatten(1, (1, 4)), hs, slots, out=row[:, 8:16])
     assert side.data_ptr() == row[:, 8:16].data_ptr()
 
 

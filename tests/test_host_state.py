@@ -46,7 +46,7 @@ for k, f in enumerate(ok): assert f() == 0, (k, L.rh_last_error(ctx))
 bad = [(INVALID, lambda: L.rh_state_conv(ctx, None, P(2), 96, P(3), None, 1, 96, 4, 1, P(4), P(5), 96)), (INVALID, lambda: conv(x=None)), (INVALID, lambda: conv(y=None)), (INVALID, lambda: conv(weight=None)),
        (INVALID, lambda: conv(state=None)), (INVALID, lambda: conv(rows(slots=None))), (INVALID, lambda: conv(t=2)), (INVALID, lambda: conv(t=7)), (SHAPE, lambda: conv(ch=0)), (SHAPE, lambda: conv(w=1)),
        (SHAPE, lambda: conv(w=9)), (SHAPE, lambda: conv(xs=95)), (SHAPE, lambda: conv(ys=95)), (SHAPE, lambda: conv(rows(8, n_rows=9))), (SHAPE, lambda: conv(rows(-1))), (SHAPE, lambda: conv(rows(n_slots=-1))),
-       (CAPACITY, lambda: conv(rows(2049, 5000))), (SHAPE, lambda: conv(rows(2 ** 31 - 1), ch=2 ** 20, xs=2 ** 20, ys=2 ** 20)), (SHAPE, lambda: conv(rows(8, -1))),
+       (CAPACITY, lambda: conv(rows(2049, 5000))), (SHAPE, lambda: conv(rows(2, 0x7FFF0001), ch=1)), (SHAPE, lambda: scan(rows(2, 0x7FFF0001))), (SHAPE, lambda: conv(rows(2 ** 31 - 1), ch=2 ** 20, xs=2 ** 20, ys=2 ** 20)), (SHAPE, lambda: conv(rows(8, -1))),
        (INVALID, lambda: L.rh_state_scan(ctx, None, C.byref(inputs()), P(8), P(10), 96)), (INVALID, lambda: L.rh_state_scan(ctx, C.byref(rows()), None, P(8), P(10), 96)),
        *[(INVALID, lambda k=k: scan(i=inputs(**{k: None}))) for k in ("x", "dt", "b", "c", "a")], (INVALID, lambda: scan(y=None)), (INVALID, lambda: scan(state=None)), (INVALID, lambda: scan(rows(slots=None))),
        (INVALID, lambda: scan(i=inputs(type=2))), (SHAPE, lambda: scan(i=inputs(channels=0))), (SHAPE, lambda: scan(i=inputs(channels=65537))), (SHAPE, lambda: scan(i=inputs(groups=0))),
@@ -54,7 +54,7 @@ bad = [(INVALID, lambda: L.rh_state_conv(ctx, None, P(2), 96, P(3), None, 1, 96,
        *[(SHAPE, lambda k=k: scan(i=inputs(**{k: 31 if k in ("b_stride", "c_stride") else 95}))) for k in ("x_stride", "dt_stride", "gate_stride", "b_stride", "c_stride")],
        (CAPACITY, lambda: scan(rows(2049, 5000))), (SHAPE, lambda: scan(rows(2 ** 31 - 1), inputs(channels=65536, x_stride=65536, dt_stride=65536, gate_stride=65536), 65536)),
        (INVALID, lambda: gated(t=2)), (SHAPE, lambda: gated(cols=0)), (SHAPE, lambda: gated(n=-1)), (SHAPE, lambda: gated(cols=32769, groups=1, xs=40000, zs=40000)), (SHAPE, lambda: gated(groups=0)),
-       (SHAPE, lambda: gated(groups=7)), (SHAPE, lambda: gated(cols=2050, groups=1025, xs=2050, zs=2050)), (SHAPE, lambda: gated(xs=95)), (SHAPE, lambda: gated(zs=95)), (INVALID, lambda: gated(eps=-1.0)),
+       (SHAPE, lambda: gated(groups=7)), (SHAPE, lambda: gated(n=2 ** 31 - 1, cols=2048, groups=1, xs=2048, zs=2048)), (SHAPE, lambda: gated(cols=2050, groups=1025, xs=2050, zs=2050)), (SHAPE, lambda: gated(xs=95)), (SHAPE, lambda: gated(zs=95)), (INVALID, lambda: gated(eps=-1.0)),
        (INVALID, lambda: gated(eps=float("nan"))), (INVALID, lambda: gated(y8=None)), (INVALID, lambda: gated(sc=None)), (INVALID, lambda: gated(y=None, y8=None, sc=None))]
 for k, (st, f) in enumerate(bad):
     rec.rec_reset()
