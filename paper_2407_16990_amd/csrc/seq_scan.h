@@ -6,9 +6,11 @@
 // Many tokens: bound by the vector instructions of h = exp2(delta a) h + delta x b, y += c h, of which the power takes twice as long as the four others: 24
 // cycles for a wave's 64 states.  A workgroup has CH channels of a stream and goes through its rows, ROWS of them staged in LDS at a time: delta and delta * x of every
 // channel, worked out once, b and c in fp32; the next rows' loads are in flight meanwhile.  y takes delta's place.  30 streams of 920 rows, 2048
-// channels of 16 states in bf16: 284 us, where the instructions of the recursion alone take 138 and the bytes 89; about a third of the others are softplus and SiLU.
+// channels of 16 states in bf16: 276 us, where the instructions of the recursion alone take 138 and the bytes 89.  A row of a workgroup's 64 channels takes each SIMD 138 cycles by
+// count, 94 of them in the recursion, the others mostly in softplus and SiLU; with eight workgroups a CU it takes 140, with the four that this call has 160.
+// (128 channels a workgroup 295 us where 64 took 286; 32 rows a stage 281, 16 329; registers for four waves a SIMD, some of them spilled, 290.)
 // Where streams are few, long ones are cut into chunks that are scanned side by side, twice: from zeros, for what they add to the state behind them, and
-// again from the state that those ahead leave.  16384 rows of one stream, 1024 channels: 158 us.
+// again from the state that those ahead leave.  16384 rows of one stream, 1024 channels: 160 us, two thirds of it in the second scan.
 #pragma once
 #define SCAN_TARGET 4            // workgroups a CU, or so, that streams are cut for
 #define SCAN_LEAST 128           // rows a chunk, at least
@@ -200,7 +202,7 @@ template <typename T, int LN, int NS> struct scan_shape {
     static constexpr int ROWS = (BY_X < BY_B ? BY_X : BY_B) < MOST ? (BY_X < BY_B ? BY_X : BY_B) : MOST;     // 32 KB of LDS for delta and delta * x, or for b and c, at most
     static constexpr int PIECES = ROWS * CH / E, NX = (PIECES + 255) / 256;              // of 16 bytes of x, a stage's and a thread's
     static constexpr int QUADS = ROWS * N / 4, NB = (QUADS + 255) / 256;                 // of b, and of c
-    static constexpr int LDS = ROWS * (CH + N) * 2 * 4;
+    static constexpr int DU = CH * 2 + 4, LDS = ROWS * (DU + N * 2) * 4;                 // words of a row of delta and delta * x: four more than it has, so that neighbouring rows begin in other banks
 };
 
 // One workgroup's rows of one stream, [first, stop), and CH channels, block blk of them.  OUT: y, and the state behind the stream's last row.  Otherwise what a chunk
@@ -211,9 +213,9 @@ template <typename T, int LN, int NS, bool FULL, bool OUT>
 __device__ __forceinline__ void scan_chunk(const scan_args& a, f32x4* s_stage, int b, int32_t place, int32_t ws_row, int32_t chunks, int32_t blk, int32_t first, int32_t stop)
 {
     typedef scan_shape<T, LN, NS> S;
-    constexpr int E = S::E, CH = S::CH, WCH = S::WCH, N = S::N, ROWS = S::ROWS, NX = S::NX, NB = S::NB, Q = NS / 4;
+    constexpr int E = S::E, CH = S::CH, WCH = S::WCH, N = S::N, ROWS = S::ROWS, NX = S::NX, NB = S::NB, DU = S::DU, Q = NS / 4;
     float* s_du = (float*)s_stage;                           // [row][channel]: delta and delta * x, then y
-    float *s_b = s_du + ROWS * CH * 2, *s_c = s_b + ROWS * N;
+    float *s_b = s_du + ROWS * DU, *s_c = s_b + ROWS * N;
     int32_t* s_odd = (int32_t*)(s_c + ROWS * N);             // unless FULL: whether any delta * x of the rows in LDS is not finite; of the next ones
 
     const int t = threadIdx.x, lane = t & 63, cl = (t >> 6) * WCH + lane % WCH, n0 = lane / WCH * NS;
@@ -240,28 +242,31 @@ __device__ __forceinline__ void scan_chunk(const scan_args& a, f32x4* s_stage, i
         }
     }
 
-    // ---- this thread's pieces of the rows: E channels, the same of every row that it has
+    // ---- this thread's pieces of the rows: E channels from cc on, the same of every row that it has.  The block's last piece ends where the block does, and so begins
+    // inside the one ahead: both give what they share the same values.  A block of fewer channels than a piece goes an element at a time.
     constexpr int PR = CH / E, RX = 256 / PR, RB = 256 / (N / 4);            // pieces a row; rows from a thread's piece, or quad of b, to its next
-    const int pc = t % PR * E, pr = t / PR, cg = c_blk + pc, left = c_end - cg, br = t / (N / 4), bn = t % (N / 4) * 4;
-    const bool narrow = c_end < E, whole = c_blk + CH <= c_end;              // fewer channels than a piece; no piece that is not a whole one
-    const int cc = narrow ? 0 : cg < c_end - E ? cg : c_end - E;             // where it is loaded from
+    // 16 neighbouring threads have pieces of several rows, whose 16 bytes at a time then lie in different banks of LDS: PN pieces of 2 * E words each, of RN rows that begin 4 words apart
+    constexpr int PN = PR < 32 / E ? PR : 32 / E, RN = 16 / PN < RX ? 16 / PN : RX;
+    const int pc = (t % PN + t / (PN * RN) % (PR / PN) * PN) * E, pr = t / PN % RN + t / (PR * RN) * RN;
+    const int cg = c_blk + pc, br = t / (N / 4), bn = t % (N / 4) * 4;
+    const bool whole = c_blk + CH <= c_end;
+    const bool few = c_end - c_blk < E;
+    const int cc = few || cg <= c_end - E ? cg : c_end - E, lc = cc - c_blk, left = c_end - cc;
     float bias[E], skip[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-        bias[e] = a.dt_bias && e < left ? a.dt_bias[cg + e] : 0.f;
-        skip[e] = OUT && a.skip && e < left ? a.skip[cg + e] : 0.f;
+        bias[e] = a.dt_bias && e < left ? a.dt_bias[cc + e] : 0.f;
+        skip[e] = OUT && a.skip && e < left ? a.skip[cc + e] : 0.f;
     }
     // where its first piece of a stage's rows lies, and its first quad
     const T *px = (const T*)a.x + ((int64_t)first + pr) * a.x_stride + cc, *pd = (const T*)a.dt + ((int64_t)first + pr) * a.dt_stride + cc;
     const T *pz = (const T*)a.gate + ((int64_t)first + pr) * a.gate_stride + cc;
     const T *pb = (const T*)a.b + ((int64_t)first + br) * a.b_stride + (int64_t)g * a.n, *pq = (const T*)a.c + ((int64_t)first + br) * a.c_stride + (int64_t)g * a.n;
-    T* py = (T*)a.y + ((int64_t)first + pr) * a.y_stride + cg;
+    T* py = (T*)a.y + ((int64_t)first + pr) * a.y_stride + cc;
     struct raw { u32x4 x[NX], dt[NX]; f32x4 b[NB], c[NB]; };
     u32x4 gate[NX];
-    auto piece = [&](const T* p) __attribute__((always_inline)) { return narrow ? row_load<T, E>(p, cg, c_end) : seq_load<u32x4>(p); };
-    auto value = [&](u32x4 w, float (&v)[E]) __attribute__((always_inline)) {
-        if (whole) row_place<T, E>(w, 0, E, v); else row_place<T, E>(w, cg, c_end, v);
-    };
+    auto piece = [&](const T* p) __attribute__((always_inline)) { return few ? row_load<T, E>(p, 0, left < 0 ? 0 : left < E ? left : E - 1) : seq_load<u32x4>(p); };
+    auto value = [&](u32x4 w, float (&v)[E]) __attribute__((always_inline)) { row_place<T, E>(w, 0, E, v); };
     // the thread's pieces (quads) of a stage: those of rows that are there; where some are not, behind the last, of the last
     auto each = [&](auto n, auto step, int r0, bool full, int rows, auto f) __attribute__((always_inline)) {
         if (full) {
@@ -309,12 +314,18 @@ __device__ __forceinline__ void scan_chunk(const scan_args& a, f32x4* s_stage, i
 #pragma unroll
                     for (int e = 0; e < E; ++e) dt[e] = scan_softplus(dt[e]);
                 }
-                f32x4* to = (f32x4*)(s_du + ((i * RX + pr) * CH + pc) * 2);
+                float* to = s_du + (i * RX + pr) * DU + lc * 2;
 #pragma unroll
-                for (int e = 0; e < E; e += 2) {
-                    const f32x4 v = {dt[e], dt[e] * x[e], dt[e + 1], dt[e + 1] * x[e + 1]};
-                    if (!FULL) odd |= !(fabsf(v[1]) < INFINITY) || !(fabsf(v[3]) < INFINITY);
-                    to[e / 2] = v;
+                for (int e = 0; e < E; ++e) {
+                    x[e] *= dt[e];
+                    if (!FULL) odd |= !(fabsf(x[e]) < INFINITY);
+                }
+                if (whole) {                                 // at 16 bytes
+#pragma unroll
+                    for (int e = 0; e < E; e += 2) *(f32x4*)(to + 2 * e) = f32x4{dt[e], x[e], dt[e + 1], x[e + 1]};
+                } else {
+#pragma unroll
+                    for (int e = 0; e < E; ++e) *(float2*)(to + 2 * e) = make_float2(dt[e], x[e]);
                 }
             }
             if (!FULL && odd) s_odd[turn] = 1;
@@ -330,7 +341,7 @@ __device__ __forceinline__ void scan_chunk(const scan_args& a, f32x4* s_stage, i
             for (int i = 0; i < NX; ++i)
                 if (i * RX + pr >= rows && (!IDLE || pr < ROWS))
 #pragma unroll
-                    for (int e = 0; e < E; e += 2) ((f32x4*)(s_du + ((i * RX + pr) * CH + pc) * 2))[e / 2] = f32x4{0.f, 0.f, 0.f, 0.f};
+                    for (int e = 0; e < E; ++e) *(float2*)(s_du + (i * RX + pr) * DU + (lc + e) * 2) = make_float2(0.f, 0.f);
 #pragma unroll
             for (int i = 0; i < NB; ++i)
                 if (i * RB + br >= rows && (!IDLE_B || br < ROWS)) *(f32x4*)(s_b + (i * RB + br) * N + bn) = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -348,7 +359,7 @@ __device__ __forceinline__ void scan_chunk(const scan_args& a, f32x4* s_stage, i
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int r = r0 + i;
-                const float2 du = *(const float2*)(s_du + (r * CH + cl) * 2);
+                const float2 du = *(const float2*)(s_du + r * DU + cl * 2);
                 float sum = 0.f;
 #pragma unroll
                 for (int q = 0; q < Q; ++q) {
@@ -374,7 +385,7 @@ __device__ __forceinline__ void scan_chunk(const scan_args& a, f32x4* s_stage, i
             if constexpr (OUT) {
                 scan_join<LN>(y);
 #pragma unroll
-                for (int i = 0; i < (LN < 4 ? 4 / LN : 1); ++i) s_du[((r0 + scan_row<LN>(i, lane)) * CH + cl) * 2] = y[i];
+                for (int i = 0; i < (LN < 4 ? 4 / LN : 1); ++i) s_du[(r0 + scan_row<LN>(i, lane)) * DU + cl * 2] = y[i];
             }
         };
         const int some = full ? ROWS : rows;
@@ -382,15 +393,20 @@ __device__ __forceinline__ void scan_chunk(const scan_args& a, f32x4* s_stage, i
         else for (int r0 = 0; r0 < some; r0 += 4) four(r0, seq_const<0>());
         __syncthreads();
         if (!FULL && t == 0) s_odd[turn] = 0;                // the rows after the next write it again, behind a barrier
-        // ---- y: the thread's own pieces, which it also fills with the next rows
+        // ---- y: the thread's own pieces, which it alone fills with the next rows (but for the block's last, see below)
         if constexpr (OUT) {
 #pragma unroll
             for (int i = 0; i < NX; ++i) {
                 if (i * RX + pr >= some) continue;
                 float y[E], z[E];
-                const f32x4* from = (const f32x4*)(s_du + ((i * RX + pr) * CH + pc) * 2);
+                const float* from = s_du + (i * RX + pr) * DU + lc * 2;
+                if (whole) {
 #pragma unroll
-                for (int e = 0; e < E; e += 2) { y[e] = from[e / 2][0]; y[e + 1] = from[e / 2][2]; }
+                    for (int e = 0; e < E; e += 2) { const f32x4 v = *(const f32x4*)(from + 2 * e); y[e] = v[0]; y[e + 1] = v[2]; }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < E; ++e) y[e] = from[2 * e];
+                }
                 if (a.skip) {
                     value(kept[i], z);
 #pragma unroll
@@ -401,10 +417,10 @@ __device__ __forceinline__ void scan_chunk(const scan_args& a, f32x4* s_stage, i
 #pragma unroll
                     for (int e = 0; e < E; ++e) y[e] *= seq_silu(z[e]);
                 }
-                if (whole) row_store<T, E>(py + i * RX * a.y_stride, E, y);
-                else if (left > 0) row_store<T, E>(py + i * RX * a.y_stride, left, y);
+                if (cg < c_end) row_store<T, E>(py + i * RX * a.y_stride, few ? left : E, y);
             }
             py += ROWS * a.y_stride;
+            if (!whole) __syncthreads();         // pieces that share places: none is filled before all have been read
         }
     }
     if constexpr (OUT) {                                     // ---- the state behind the last row
