@@ -3,7 +3,7 @@
 // Bound by memory: x and the gate are read once, y and its 8-bit form written once.  A row belongs to one workgroup, a group of it to `lanes`
 // neighbouring threads, with ITEMS pieces of 16 bytes a thread; pieces begin where groups do, at any address.  A row of more groups than the
 // threads are for goes ROUNDS times around.  The products stay in registers between the sums of squares, the largest |y| of the row and the output.
-// 27600 rows of 2048 in 8 groups of bf16, both outputs, inputs that no cache holds: 90 us, 4.4 TB/s; 14720 of 1540 in 4 groups of fp32 53, 5.1 TB/s; 8 of 2048, 8-bit output, 4.1.
+// 27600 rows of 2048 in 8 groups of bf16, both outputs, inputs that no cache holds: 86 us, 4.6 TB/s; 14720 of 1540 in 4 groups of fp32 53, 5.1 TB/s; 8 of 2048, 8-bit output, 4.1.
 // Several rows a workgroup, one after the other with the next one's loads ahead: 95 and 63 (two), 92 and 71 (four).
 #include "seq_rows.h"
 #include "seq_streams.h"

@@ -10,7 +10,7 @@
 // count, 94 of them in the recursion, the others mostly in softplus and SiLU; with eight workgroups a CU it takes 140, with the four that this call has 160.
 // (128 channels a workgroup 295 us where 64 took 286; 32 rows a stage 281, 16 329; registers for four waves a SIMD, some of them spilled, 290.)
 // Where streams are few, long ones are cut into chunks that are scanned side by side, twice: from zeros, for what they add to the state behind them, and
-// again from the state that those ahead leave.  16384 rows of one stream, 1024 channels: 160 us, two thirds of it in the second scan.
+// again from the state that those ahead leave.  16384 rows of one stream, 1024 channels: 77 us and 88.
 #pragma once
 #define SCAN_TARGET 4            // workgroups a CU, or so, that streams are cut for
 #define SCAN_LEAST 128           // rows a chunk, at least
@@ -389,8 +389,10 @@ __device__ __forceinline__ void scan_chunk(const scan_args& a, f32x4* s_stage, i
             }
         };
         const int some = full ? ROWS : rows;
+        __builtin_amdgcn_s_setprio(1);                       // ahead of waves that stage: 37 ragged streams 216 -> 205 us, 64 of 64 states 102 -> 98
         if (!FULL && s_odd[turn]) for (int r0 = 0; r0 < some; r0 += 4) four(r0, seq_const<1>());
         else for (int r0 = 0; r0 < some; r0 += 4) four(r0, seq_const<0>());
+        __builtin_amdgcn_s_setprio(0);
         __syncthreads();
         if (!FULL && t == 0) s_odd[turn] = 0;                // the rows after the next write it again, behind a barrier
         // ---- y: the thread's own pieces, which it alone fills with the next rows (but for the block's last, see below)
