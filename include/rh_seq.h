@@ -16,7 +16,7 @@
  * stream, arguments checked before any launch, rh_last_error.  They use neither the context's network nor its capacities,
  * and count in no class of rh_profile_read.  Sums, softmax statistics and norms are held in 32 bits.
  * Scratch memory of rh_cache_attend, rh_matvec_packed and rh_state_scan (68 MB on 256 CUs) and a few counters, of rh_cache_plan too, belong to the context: the first call that wants
- * them allocates them and waits for the stream, and no later one does.  Graphs may be recorded once an rh_cache_attend or rh_matvec_packed call, or an rh_state_scan call of more than one token a stream, of the context has been made
+ * them allocates them and waits for the stream, and no later one does.  Graphs may be recorded once an rh_cache_attend or rh_matvec_packed call, or the rh_state_scan call to be recorded, has been made on the context
  * (RH_E_STATE where a captured call would have to allocate).  Since calls share this memory, those of one context must not overlap on two streams, replays of
  * a graph that recorded them among them: use a context for each, or let one wait for the other.
  */
