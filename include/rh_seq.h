@@ -158,7 +158,7 @@ rh_status rh_state_conv(rh_ctx* ctx, const rh_state_rows* rows, const void* x, i
  *   y[t][c] = sum_i c[t][g][i] * h[c][i] + skip[c] * x[t][c], with a gate times gate[t][c] / (1 + exp(-gate[t][c]))
  *   x, dt, gate (NULL: none) and y (dev): `type` (RH_T_F32 or RH_T_BF16), rows x_stride ... y_stride elements apart (>= channels); y overlaps none of the inputs.
  *   b, c (dev): `type`, element (t, g, i) at t*b_stride + g*n + i (b_stride, c_stride >= groups*n).
- *   a (dev) f32 [channels][n]; dt_bias, skip (dev) f32 [channels], each may be NULL; channels <= RH_SEQ_MAX_CHANNELS, 1 <= n <= RH_SEQ_MAX_STATE; groups divides channels.
+ *   a (dev) f32 [channels][n], beyond 2.3e38 taken as that; dt_bias, skip (dev) f32 [channels], each may be NULL; channels <= RH_SEQ_MAX_CHANNELS, 1 <= n <= RH_SEQ_MAX_STATE; groups divides channels.
  *   state (dev, in/out) f32 [n_slots][channels][n].
  * Streams that are long for the call are cut into chunks, which are scanned side by side: from zeros first, for what each adds to the state
  * behind it, and again from the state that the chunks ahead leave.  Sums come in the same order every time.

@@ -6,7 +6,7 @@
 // Many tokens: bound by the vector instructions of h = exp2(delta a) h + delta x b, y += c h, of which the power takes twice as long as the four others: 24
 // cycles for a wave's 64 states.  A workgroup has CH channels of a stream and goes through its rows, ROWS of them staged in LDS at a time: delta and delta * x of every
 // channel, worked out once, b and c in fp32; the next rows' loads are in flight meanwhile.  y takes delta's place.  30 streams of 920 rows, 2048
-// channels of 16 states in bf16: 276 us, where the instructions of the recursion alone take 138 and the bytes 89.  A row of a workgroup's 64 channels takes each SIMD 138 cycles by
+// channels of 16 states in bf16: 279 us, where the instructions of the recursion alone take 138 and the bytes 89.  A row of a workgroup's 64 channels takes each SIMD 138 cycles by
 // count, 94 of them in the recursion, the others mostly in softplus and SiLU; with eight workgroups a CU it takes 140, with the four that this call has 160.
 // (128 channels a workgroup 295 us where 64 took 286; 32 rows a stage 281, 16 329; registers for four waves a SIMD, some of them spilled, 290.)
 // Where streams are few, long ones are cut into chunks that are scanned side by side, twice: from zeros, for what they add to the state behind them, and
@@ -16,6 +16,7 @@
 #define SCAN_LEAST 128           // rows a chunk, at least
 #define SCAN_ROWS 64             // rows a stage, at most
 #define SCAN_WHOLE 0x3FFFFFFF    // rows a chunk that no stream's are one and a half times
+#include <float.h>
 #include "seq_rows.h"
 #include "seq_streams.h"
 
@@ -102,6 +103,15 @@ template <bool FULL> __device__ __forceinline__ void scan_put(float* p, int i, i
         for (int e = 0; e < 4; ++e) if (i + e < n) p[i + e] = v[e];
 }
 
+// a * log2(e), finite where a is: times a delta of 0, a row behind the last among them, it leaves the state as it is
+__device__ __forceinline__ f32x4 scan_fade(f32x4 a)
+{
+    f32x4 v = a * 1.44269504089f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = fabsf(v[e]) == INFINITY ? copysignf(FLT_MAX, v[e]) : v[e];
+    return v;
+}
+
 // ---------------------------------------------------------------------------------------------------------------
 // one row a stream
 // ---------------------------------------------------------------------------------------------------------------
@@ -130,7 +140,7 @@ __global__ __launch_bounds__(256) void k_seq_scan_step(scan_args a)
         dt[i] = seq_to_f32(((const T*)a.dt)[s * a.dt_stride + c]);
         gate[i] = a.gate ? seq_to_f32(((const T*)a.gate)[s * a.gate_stride + c]) : 0.f;
     }
-    const f32x4 fade = scan_quad<float, FULL>(a.a + at, 4 * j, a.n) * 1.44269504089f;
+    const f32x4 fade = scan_fade(scan_quad<float, FULL>(a.a + at, 4 * j, a.n));
     const float bias = a.dt_bias ? a.dt_bias[c] : 0.f, skip = a.skip ? a.skip[c] : 0.f;
 #pragma unroll
     for (int i = 0; i < R; ++i) {
@@ -235,7 +245,7 @@ __device__ __forceinline__ void scan_chunk(const scan_args& a, f32x4* s_stage, i
 #pragma unroll
         for (int q = 0; q < Q; ++q) {
             const int n = n0 + 4 * q;
-            fade[q] = scan_quad<float, FULL>(a.a + at, n, a.n) * 1.44269504089f;
+            fade[q] = scan_fade(scan_quad<float, FULL>(a.a + at, n, a.n));
             h[q] = f32x4{0.f, 0.f, 0.f, 0.f};
             if (OUT && chunks > 1) h[q] = *(const f32x4*)(a.ws + ((int64_t)(ws_row + place) * a.channels + cs) * N + n);
             else if (OUT && from >= 0) h[q] = scan_quad<float, FULL>(a.state + from * pool + at, n, a.n);
@@ -483,9 +493,11 @@ __device__ __forceinline__ void scan_chunk(const scan_args& a, f32x4* s_stage, i
                     const f32x4 more = __builtin_bit_cast(f32x4, add[i]);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        // what fades to nothing over a chunk, step by step was more each time: an infinite state stays infinite
-                        const float f = __builtin_amdgcn_exp2f(__uint_as_float(sum[i]) * fade[q][e]);
-                        v[e] = fmaf(f == 0.f ? 0x1p-149f : f, v[e], more[e]);
+                        // Step by step no power was 0 or infinite, whatever all of them make: in two halves, which neither are, an infinite state stays infinite,
+                        // one of zeros zero, and a small one may grow by more than 2^128.
+                        float f = __builtin_amdgcn_exp2f(0.5f * __uint_as_float(sum[i]) * fade[q][e]);
+                        f = f == 0.f ? 0x1p-149f : f > FLT_MAX ? FLT_MAX : f;
+                        v[e] = fmaf(f, f * v[e], more[e]);
                         if (!FULL && n0 + 4 * q + e >= a.n) v[e] = 0.f;                  // a state that is none: an infinite sum times its zero
                     }
                 }

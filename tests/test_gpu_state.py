@@ -698,3 +698,46 @@ def test_results_do_not_change_from_run_to_run(rh):
         states = torch.zeros((3, 3, 200), dtype=torch.bfloat16, device="cuda"), torch.zeros((3, 200, 16), device="cuda")
         runs.append([v.clone().view(torch.uint8) for v in (*step(t, *states, slots, **kw), *states)])
     assert all(torch.equal(p, q) for r in runs[1:] for p, q in zip(runs[0], r))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n", [5, 16])
+def test_scan_decays_of_the_largest_size(rh, dtype, n):
+    """a of -3e38: a step of 0 leaves the state, one of 1 leaves nothing of it; rows behind a stream's last are no steps."""
+    channels, low = 6, -3e38
+    for lens in ([5, 2, 301], [801], None):
+        s = Streams(np.random.default_rng(2), lens, 3)
+        i = _scan_inputs(_gen(4), s, channels, n, 1, dtype, dt_bias=False, gate=False, skip=False)
+        i = {k: v if v is None else v.clone() for k, v in i.items()}
+        i["a"] = torch.full_like(i["a"], low)
+        i["dt"] = (torch.rand(i["dt"].shape, generator=_gen(6), device="cuda") < 0.2).to(dtype)
+        state = i.pop("state")
+        p = {k: None if v is None else _np(v) for k, v in i.items()}
+        want, new, most = O.scan(**p, state=_np(state), soft=False, **s.plain())
+        y = rh.state_scan(**i, state=state, slots=s.slots, softplus=False, **s.kw())
+        k = s.keep
+        # the state is a product rounded once or what it was: U; n products and sums of y, and its own rounding
+        assert (np.abs(_np(y)[k] - want[k]) <= (n + 4) * U * most[k] + HALF[dtype] * np.abs(want[k]) * (1 + 2 * n * U) + 2 * n * U * most[k] + TINY).all()
+        assert (np.abs(_np(state) - new) <= 2 * U * np.abs(new) + TINY).all()
+
+
+@pytest.mark.parametrize("n", [5, 16])
+def test_scan_states_that_grow_past_the_powers(rh, n):
+    """a above 0 over chunks whose power passes 2^128: a state of zeros stays so until something is added, a small one grows to what it is step by step."""
+    channels, rows = 3, 400                                          # chunks of 128 rows or more; exp(0.75 * 128) passes 2^128
+    s = Streams(np.random.default_rng(2), [rows])
+    i = _scan_inputs(_gen(4), s, channels, n, 1, torch.float32, dt_bias=False, gate=False, skip=False)
+    i = {k: v if v is None else v.clone() for k, v in i.items()}
+    i["a"] = torch.full_like(i["a"], 1.0)
+    i["dt"] = torch.zeros_like(i["dt"])
+    i["dt"][:150, 0], i["dt"][:, 1], i["dt"][:, 2] = 0.75, 0.75, 0.0
+    i["x"][:-1] = 0
+    state = torch.zeros_like(i.pop("state"))
+    state[int(s.slots[0]), 0] = 1e-30
+    p = {k: None if v is None else _np(v) for k, v in i.items()}
+    want, new, most = O.scan(**p, state=_np(state), soft=False, **s.plain())
+    assert np.isfinite(want).all()
+    y = rh.state_scan(**i, state=state, slots=s.slots, softplus=False, **s.kw())
+    # a step's power is off by 4 U and 0.75 * log2(e) * U ln 2 of its argument, rounded once; a chunk's by its sum's 112 and both halves: 6 a step are above either
+    assert (np.abs(_np(y) - want) <= (150 * 6 + n + 4) * U * most + TINY).all()
+    assert (np.abs(_np(state) - new) <= (150 * 6 + 4) * U * np.abs(new) + TINY).all()
