@@ -12,10 +12,14 @@
 // Where streams are few, long ones are cut into chunks that are scanned side by side, twice: from zeros, for what they add to the state behind them, and
 // again from the state that those ahead leave.  16384 rows of one stream, 1024 channels: 77 us and 88.
 #pragma once
-#define SCAN_TARGET 4            // workgroups a CU, or so, that streams are cut for
-#define SCAN_LEAST 128           // rows a chunk, at least
+// us, channels of 16 states in bf16 unless said otherwise.  SCAN_TARGET 2, 3, 4: 16384 rows of one stream, 1024 channels, 155, 160, 163; 37 of up to 2000, 522 of 13 in fp32, 240, 205, 217;
+// 8 of 600, 1024, 59.5, 52, 52; 8 of 1000, 1024 of 128, 240, 240, 348; 12 of up to 3000, 1024, 178, 157, 177.  SCAN_LEAST 128: one of 300, 1024, 33.1 for 21.7; one of 1000, 2048, 36.1 for 31.7.
+// Cut and whole: one of 230, 1024, 21.8 and 26.8; 8 of 230 30.6 and 31.6; 16 of 230 45 and 34; 30 of 250 65 and 46.
+#define SCAN_TARGET 3            // workgroups a CU, or so, that streams are cut for
+#define SCAN_LEAST 64            // rows a chunk, at least
 #define SCAN_ROWS 64             // rows a stage, at most
-#define SCAN_WHOLE 0x3FFFFFFF    // rows a chunk that no stream's are one and a half times
+#define SCAN_CUT 288             // rows of a stream that is cut, at least
+#define SCAN_WHOLE 0x7FFFFFC0    // rows a chunk that no stream has
 #include <float.h>
 #include "seq_rows.h"
 #include "seq_streams.h"
@@ -167,13 +171,13 @@ __global__ __launch_bounds__(256) void k_seq_scan_step(scan_args a)
 // ---------------------------------------------------------------------------------------------------------------
 // many rows a stream
 // ---------------------------------------------------------------------------------------------------------------
-// A stream of `len` rows is cut into chunks of equal length, a.chunk rows or so; below one and a half it stays whole.
+// A stream of `len` rows is cut into chunks of equal length, a.chunk rows (whole stages) at most; below one and a half of them, or SCAN_CUT rows, it stays whole.
 template <int ROWS> struct scan_cut {
     int32_t size, n;
     __device__ __forceinline__ scan_cut(int32_t len, int32_t chunk)
     {
-        n = (int32_t)(((uint32_t)len + (uint32_t)chunk / 2) / (uint32_t)chunk);
-        if (n < 2) { size = len; n = len > 0; return; }
+        if (len < SCAN_CUT || (uint32_t)len < (uint32_t)chunk + (uint32_t)chunk / 2) { size = len; n = len > 0; return; }
+        n = (int32_t)(((uint32_t)len + (uint32_t)chunk - 1) / (uint32_t)chunk);
         size = (int32_t)(((uint32_t)len + n - 1) / (uint32_t)n + ROWS - 1) / ROWS * ROWS;
         n = (int32_t)(((uint32_t)len + size - 1) / (uint32_t)size);                         // rounded up to whole stages, fewer may do
     }
@@ -530,6 +534,7 @@ static hipError_t launch_scan(rh_ctx* ctx, scan_args& a, rh_status* failed)
     const int64_t wide = (a.channels + 256 / LN - 1) / (256 / LN);           // workgroups of one channel a thread
     if (!a.r.offsets) {
         a.blocks = seq_make_div((uint32_t)wide);
+        // four streams a thread and one, us: 512 of 4096 channels 57 and 71, 256 of 1024 10.0 and 9.9, 64 of 2048 7.1 and 6.2, 8 of 1024 4.9 and 3.9
         if (wide * a.r.n_rows >= 16 * (int64_t)ctx->n_cu) hipLaunchKernelGGL((k_seq_scan_step<T, LN, FULL, 4>), dim3((unsigned)(((int64_t)a.r.n_rows + 3) / 4 * wide)), dim3(256), 0, ctx->stream, a);
         else hipLaunchKernelGGL((k_seq_scan_step<T, LN, FULL, 1>), dim3((unsigned)(a.r.n_rows * wide)), dim3(256), 0, ctx->stream, a);
         return hipGetLastError();
@@ -539,15 +544,16 @@ static hipError_t launch_scan(rh_ctx* ctx, scan_args& a, rh_status* failed)
     a.blocks = seq_make_div((uint32_t)blocks);
     a.group_blocks = seq_make_div((uint32_t)group_blocks);
     // Rows a chunk: enough workgroups for the GPU where streams are few, and no more states than the scratch memory holds.  Nothing is cut where the channels alone are enough:
-    // so (4/3 rows / chunk + 1) * blocks, the counters that there may be, stay below 5.4 + 4 a CU of the 16.
+    // so (3/2 rows / chunk + 1) * blocks, the counters that there may be, stay below 4.5 + 4 a CU of the 16.
     const int64_t room = SCAN_ROOM(ctx) / ((int64_t)a.channels * (S::N + 1));
-    const int64_t least = room > 0 ? (int64_t)a.r.n_rows * 4 / (3 * room) + 1 : SCAN_WHOLE;
+    const int64_t least = room > 0 ? (int64_t)a.r.n_rows * 3 / (2 * room) + 1 : SCAN_WHOLE;
     int64_t chunk = (int64_t)a.r.n_rows * blocks / (SCAN_TARGET * ctx->n_cu);
     chunk = chunk < SCAN_LEAST ? SCAN_LEAST : chunk;
     chunk = chunk < least ? least : chunk;
+    chunk = (chunk + S::ROWS - 1) / S::ROWS * S::ROWS;
     a.chunk = (int32_t)(chunk > SCAN_WHOLE || blocks > 4 * ctx->n_cu ? SCAN_WHOLE : chunk);
-    const bool cut = 2 * (int64_t)a.r.n_rows >= 3 * (int64_t)a.chunk;        // otherwise no stream can be as long
-    a.ws_rows = cut ? (int32_t)((int64_t)a.r.n_rows * 4 / (3 * (int64_t)a.chunk)) + 1 : 0;
+    const bool cut = a.r.n_rows >= SCAN_CUT && 2 * (int64_t)a.r.n_rows >= 3 * (int64_t)a.chunk;        // otherwise no stream can be as long
+    a.ws_rows = cut ? (int32_t)((int64_t)a.r.n_rows * 3 / (2 * (int64_t)a.chunk)) + 1 : 0;
     const size_t counts = a.r.n_streams > 64 ? (2 * (a.r.n_streams + 1) + STREAMS_T / 64) * sizeof(int32_t) : 0, stage = S::LDS + (FULL ? 0 : 2 * sizeof(int32_t));
     const size_t lds = stage > counts ? stage : counts;
     if (cut) {

@@ -724,13 +724,13 @@ def test_scan_decays_of_the_largest_size(rh, dtype, n):
 @pytest.mark.parametrize("n", [5, 16])
 def test_scan_states_that_grow_past_the_powers(rh, n):
     """a above 0 over chunks whose power passes 2^128: a state of zeros stays so until something is added, a small one grows to what it is step by step."""
-    channels, rows = 3, 400                                          # chunks of 128 rows or more; exp(0.75 * 128) passes 2^128
+    channels, rows = 3, 400                                          # chunks of 64 rows; exp(2 * 60) passes 2^128
     s = Streams(np.random.default_rng(2), [rows])
     i = _scan_inputs(_gen(4), s, channels, n, 1, torch.float32, dt_bias=False, gate=False, skip=False)
     i = {k: v if v is None else v.clone() for k, v in i.items()}
     i["a"] = torch.full_like(i["a"], 1.0)
     i["dt"] = torch.zeros_like(i["dt"])
-    i["dt"][:150, 0], i["dt"][:, 1], i["dt"][:, 2] = 0.75, 0.75, 0.0
+    i["dt"][:60, 0], i["dt"][:, 1], i["dt"][:, 2] = 2.0, 2.0, 0.0
     i["x"][:-1] = 0
     state = torch.zeros_like(i.pop("state"))
     state[int(s.slots[0]), 0] = 1e-30
@@ -738,6 +738,7 @@ def test_scan_states_that_grow_past_the_powers(rh, n):
     want, new, most = O.scan(**p, state=_np(state), soft=False, **s.plain())
     assert np.isfinite(want).all()
     y = rh.state_scan(**i, state=state, slots=s.slots, softplus=False, **s.kw())
-    # a step's power is off by 4 U and 0.75 * log2(e) * U ln 2 of its argument, rounded once; a chunk's by its sum's 112 and both halves: 6 a step are above either
-    assert (np.abs(_np(y) - want) <= (150 * 6 + n + 4) * U * most + TINY).all()
-    assert (np.abs(_np(state) - new) <= (150 * 6 + 4) * U * np.abs(new) + TINY).all()
+    # a step's power: its argument, 2 log2(e), rounded with log2(e) and as a product, 4 U of the power; 2 U from the power, 1 as it is multiplied.  A chunk's: its sum is exact, the
+    # argument of a half 60 log2(e), 120 U of it, twice.  8 a step are above either.
+    assert (np.abs(_np(y) - want) <= (60 * 8 + n + 4) * U * most + TINY).all()
+    assert (np.abs(_np(state) - new) <= (60 * 8 + 4) * U * np.abs(new) + TINY).all()
