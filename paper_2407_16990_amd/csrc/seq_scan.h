@@ -46,9 +46,11 @@ __device__ __forceinline__ float scan_exp(float v)
     return fmaf(e, lo * 0.69314718056f, e);
 }
 // log(1 + exp(v)): with w = 1 + e rounded, log(w) * e / (w - 1) makes up for the rounding (Goldberg 1991, theorem 4); where w is 1 the 2^-100 leave e.
-// Never below v, which it is where e is infinite and the quotient no number.
+// Never below v, which it is where e is infinite and the quotient no number.  A v below -104, whose power is 0 in 32 bits, counts as -104, so that a step masked by -inf or by a
+// type's lowest value is 0; by a comparison, which a v that is no number passes.
 __device__ __forceinline__ float scan_softplus(float v)
 {
+    v = v < -104.f ? -104.f : v;
     const float e = scan_exp(v), w = 1.f + e;
     const float l = fmaf(__builtin_amdgcn_logf(w), 0.69314718056f, 0x1p-100f), d = fmaxf(w - 1.f, 0x1p-100f);
     return fmaxf(l * (e * __builtin_amdgcn_rcpf(d)), v);
