@@ -90,7 +90,7 @@ class StreamPredictor:
     """The state of max_streams streams and the step that takes one frame of each.  rh: the context whose stream the work goes
     on, and which is to be torch's current one; other calls of that context must not overlap with a step on another stream, replays included.
     graph: record the step at its second call and replay it from then on (one launch instead of one per operator).
-    lengths: frames of each stream that found room since it began (with the mixer "state" every frame does); granted: which streams' frames did in the last step."""
+    lengths: frames of each stream that found room since it began (with the mixer "state" every frame does); granted: which streams' frames did in the last step or chunk."""
 
     def __init__(self, rh: RH, cfg: PredictorConfig, weights: dict, graph: bool = False):
         self.rh, self.cfg, dev = rh, cfg, rh.device
@@ -222,11 +222,22 @@ class StreamPredictor:
 
     def chunk(self, features: torch.Tensor, offsets: torch.Tensor) -> torch.Tensor:
         """Many frames of each stream at once (mixer "state"): features f32 [rows, n_features], rows offsets[b] to offsets[b + 1] (int32 [max_streams + 1], ascending
-        from 0 to rows) being the next frames of stream b, which goes on from them -> scores f32 [rows, mbh, mbw].  Not recorded."""
+        from 0 to rows) being the next frames of stream b, which goes on from them -> scores f32 [rows, mbh, mbw].  Not recorded.
+        As the operators take them: offsets outside [0, rows] count as its ends, where any descend no stream has a frame, and frames of no stream score 0.  At most
+        2048 streams (a step takes any number)."""
         if self.cfg.mixer != "state":
             raise ValueError("chunk: frames of a stream go one at a time through attention")
+        rows, streams = features.shape[0], self.cfg.max_streams
+        if tuple(offsets.shape) != (streams + 1,) or offsets.dtype != torch.int32:
+            raise ValueError(f"chunk: offsets {offsets.dtype} {tuple(offsets.shape)}, not torch.int32 {(streams + 1,)}")
+        offsets = offsets.clamp(0, rows)
+        offsets.mul_((offsets[1:] >= offsets[:-1]).all())
         scores = self._layers(features, self._state, self.every, offsets)
-        self.lengths.add_(offsets[1:] - offsets[:-1])
+        row = torch.arange(rows, dtype=torch.int32, device=offsets.device)
+        scores.masked_fill_(((row < offsets[0]) | (row >= offsets[-1]))[:, None, None], 0)   # their rows were never written
+        frames = offsets[1:] - offsets[:-1]
+        self.granted = frames > 0
+        self.lengths.add_(frames)
         return scores
 
     def _record(self):
