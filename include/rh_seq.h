@@ -135,6 +135,7 @@ rh_status rh_matvec_packed(rh_ctx* ctx, const void* x, int32_t x_type, int64_t x
  *     that the one before may stay.  A slot outside [0, n_slots): a state of zeros; an `into` outside: not kept.
  *   past i32 [n_streams] (NULL: all have one): 0 or below where a stream begins with this call: its state before is zeros, whatever its slot holds.
  * A stream without rows has nothing of its states read or written.  Streams may share a slot that they read; what one writes no other reads or writes.
+ * A call that is more than a launch takes is refused (RH_E_SHAPE) before any work; the entries say how much that is.
  */
 typedef struct {
     const int32_t *offsets, *slots, *into, *past;
@@ -162,6 +163,8 @@ rh_status rh_state_conv(rh_ctx* ctx, const rh_state_rows* rows, const void* x, i
  *   state (dev, in/out) f32 [n_slots][channels][n].
  * Streams that are long for the call are cut into chunks, which are scanned side by side: from zeros first, for what each adds to the state
  * behind it, and again from the state that the chunks ahead leave.  Sums come in the same order every time.
+ * A launch takes 2^24 - 1 workgroups, each of 1024 / m channels, m being n rounded up to a power of two from 4 to 64: of four streams without offsets (8 channels of
+ * more than 64 states), of one stream and one group with offsets (16 of more than 64 states).
  */
 typedef struct {
     const void *x, *dt, *gate, *b, *c;

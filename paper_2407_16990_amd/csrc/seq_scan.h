@@ -527,6 +527,13 @@ __global__ __launch_bounds__(256, 2) void k_seq_scan(scan_args a)
     scan_chunk<T, LN, NS, FULL, OUT>(a, s_stage, b, place, ws_row, cut.n, (int32_t)blk, first, stop);
 }
 
+// a launch has fewer than 2^32 threads
+static rh_status scan_fits(rh_ctx* ctx, const scan_args& a, int64_t workgroups)
+{
+    if (workgroups > 0xFFFFFF) RH_FAIL(ctx, RH_E_SHAPE, "rh_state_scan: %d rows of %d streams and %d channels are %lld workgroups (at most %d)", a.r.n_rows, a.r.n_streams, a.channels, (long long)workgroups, 0xFFFFFF);
+    return RH_OK;
+}
+
 template <typename T, int LN, bool FULL>
 static hipError_t launch_scan(rh_ctx* ctx, scan_args& a, rh_status* failed)
 {
@@ -537,8 +544,11 @@ static hipError_t launch_scan(rh_ctx* ctx, scan_args& a, rh_status* failed)
     if (!a.r.offsets) {
         a.blocks = seq_make_div((uint32_t)wide);
         // four streams a thread and one, us: 512 of 4096 channels 57 and 71, 256 of 1024 10.0 and 9.9, 64 of 2048 7.1 and 6.2, 8 of 1024 4.9 and 3.9
-        if (wide * a.r.n_rows >= 16 * (int64_t)ctx->n_cu) hipLaunchKernelGGL((k_seq_scan_step<T, LN, FULL, 4>), dim3((unsigned)(((int64_t)a.r.n_rows + 3) / 4 * wide)), dim3(256), 0, ctx->stream, a);
-        else hipLaunchKernelGGL((k_seq_scan_step<T, LN, FULL, 1>), dim3((unsigned)(a.r.n_rows * wide)), dim3(256), 0, ctx->stream, a);
+        const bool four = wide * a.r.n_rows >= 16 * (int64_t)ctx->n_cu;
+        const int64_t workgroups = (four ? ((int64_t)a.r.n_rows + 3) / 4 : a.r.n_rows) * wide;
+        if ((*failed = scan_fits(ctx, a, workgroups)) != RH_OK) return hipSuccess;
+        if (four) hipLaunchKernelGGL((k_seq_scan_step<T, LN, FULL, 4>), dim3((unsigned)workgroups), dim3(256), 0, ctx->stream, a);
+        else hipLaunchKernelGGL((k_seq_scan_step<T, LN, FULL, 1>), dim3((unsigned)workgroups), dim3(256), 0, ctx->stream, a);
         return hipGetLastError();
     }
     const int group_blocks = ((int)a.per.d + S::CH - 1) / S::CH;
@@ -558,19 +568,20 @@ static hipError_t launch_scan(rh_ctx* ctx, scan_args& a, rh_status* failed)
     a.ws_rows = cut ? (int32_t)((int64_t)a.r.n_rows * 3 / (2 * (int64_t)a.chunk)) + 1 : 0;
     const size_t counts = a.r.n_streams > 64 ? (2 * (a.r.n_streams + 1) + STREAMS_T / 64) * sizeof(int32_t) : 0, stage = S::LDS + (FULL ? 0 : 2 * sizeof(int32_t));
     const size_t lds = stage > counts ? stage : counts;
+    const int64_t workgroups = ((int64_t)a.r.n_rows / a.chunk + a.r.n_streams) * blocks;      // as many as any offsets give; the first launch has no more
+    if ((*failed = scan_fits(ctx, a, workgroups)) != RH_OK) return hipSuccess;
     if (cut) {
         rh_status st = seq_counters(ctx);
         if (st == RH_OK) st = seq_scratch(ctx);
         if (st != RH_OK) { *failed = st; return hipSuccess; }
         a.ws = (float*)ctx->seq_ws; a.count = ctx->seq_cnt;
     }
-    // as many workgroups as any offsets give
     if (cut) {
         hipLaunchKernelGGL((k_seq_scan<T, WL, NS, FULL, false>), dim3((unsigned)(((int64_t)a.r.n_rows / a.chunk + 1) * blocks)), dim3(256), lds, ctx->stream, a);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    hipLaunchKernelGGL((k_seq_scan<T, WL, NS, FULL, true>), dim3((unsigned)(((int64_t)a.r.n_rows / a.chunk + a.r.n_streams) * blocks)), dim3(256), lds, ctx->stream, a);
+    hipLaunchKernelGGL((k_seq_scan<T, WL, NS, FULL, true>), dim3((unsigned)workgroups), dim3(256), lds, ctx->stream, a);
     return hipGetLastError();
 }
 

@@ -20,9 +20,6 @@ extern "C" rh_status rh_state_scan(rh_ctx* ctx, const rh_state_rows* rows, const
         RH_FAIL(ctx, RH_E_SHAPE, "rh_state_scan: a row stride of b or c below %lld", (long long)in->groups * in->n);
     if (rows->n_rows == 0 || rows->n_streams == 0) return RH_OK;
     if (!in->x || !in->dt || !in->b || !in->c || !in->a || !y || (rows->n_slots && !state)) RH_FAIL(ctx, RH_E_INVALID, "rh_state_scan: null argument");
-    // workgroups, of which a launch has fewer than 2^24: eight channels or more each; of a group the last may have fewer
-    if (((int64_t)rows->n_rows / (rows->offsets ? 128 : 1) + rows->n_streams) * ((in->channels + 7) / 8 + (int64_t)in->groups) > 0xFFFFFFll)
-        RH_FAIL(ctx, RH_E_SHAPE, "rh_state_scan: %d rows of %d channels in %d groups", rows->n_rows, in->channels, in->groups);
     a.x = in->x; a.dt = in->dt; a.gate = in->gate; a.b = in->b; a.c = in->c; a.a = in->a; a.dt_bias = in->dt_bias; a.skip = in->skip;
     a.state = state; a.ws = nullptr; a.y = y; a.x_stride = in->x_stride; a.dt_stride = in->dt_stride; a.gate_stride = in->gate_stride;
     a.b_stride = in->b_stride; a.c_stride = in->c_stride; a.y_stride = y_stride; a.per = seq_make_div((uint32_t)(in->channels / in->groups));
