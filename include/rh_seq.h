@@ -148,6 +148,7 @@ typedef struct {
  *   x, y (dev): `type` (RH_T_F32 or RH_T_BF16), rows x_stride and y_stride elements apart (>= channels); they must not overlap.
  *   weight (dev) f32 [width][channels], 2 <= width <= RH_SEQ_MAX_TAPS; bias (dev) f32 [channels] or NULL.
  *   state (dev, in/out): `type`, [n_slots][width-1][channels]: the last inputs, the latest last.
+ * A launch takes 2^31 - 2^12 pieces of 16 bytes, of rows without offsets, of runs of 8 rows or more with them.
  */
 rh_status rh_state_conv(rh_ctx* ctx, const rh_state_rows* rows, const void* x, int64_t x_stride, const float* weight,
                         const float* bias, int32_t type, int32_t channels, int32_t width, int32_t silu, void* state,
@@ -179,6 +180,7 @@ rh_status rh_state_scan(rh_ctx* ctx, const rh_state_rows* rows, const rh_scan_in
  *   s = x * gate / (1 + exp(-gate)),  y = s * weight / sqrt(mean over its group(s^2) + eps)
  * Outputs y (in `type`) and y8 with y8_scale as in rh_norm_residual, dense; each may be NULL but not all.  x and gate have a row stride each
  * (elements, >= n_cols).  weight (dev) f32 [n_cols]; groups <= RH_SEQ_MAX_GROUPS divides n_cols.
+ * A launch takes 2^32 - 1 threads; a row has 1024 at most, and at most four for every 16 bytes of a group.
  */
 rh_status rh_norm_gated(rh_ctx* ctx, const void* x, int64_t x_stride, const void* gate, int64_t gate_stride, const float* weight,
                         int32_t type, int32_t n_rows, int32_t n_cols, int32_t groups, float eps, void* y, uint8_t* y8,

@@ -234,7 +234,7 @@ extern "C" rh_status rh_state_conv(rh_ctx* ctx, const rh_state_rows* rows, const
     // 59 and 53 (32 leave three workgroups and a half a CU); 37 of up to 1500, 515 in fp32 29.3, 26.4, 29.1 and 40.5.
     a.log_run = ((int64_t)rows->n_rows >> 4) * pieces < (int64_t)ctx->n_cu * 2 * STREAMS_T ? 3 : 4;
     a.run = 1 << a.log_run;
-    if (((int64_t)rows->n_rows / (rows->offsets ? a.run : 1) + rows->n_streams) * pieces > 0x7FFFF000ll)
+    if ((rows->offsets ? (int64_t)rows->n_rows / a.run + rows->n_streams : rows->n_rows) * pieces > 0x7FFFF000ll)
         RH_FAIL(ctx, RH_E_SHAPE, "rh_state_conv: %d rows of %d channels", rows->n_rows, channels);
     a.x = x; a.weight = weight; a.bias = bias; a.state = state; a.y = y; a.x_stride = x_stride; a.y_stride = y_stride;
     a.pieces = seq_make_div((uint32_t)pieces); a.channels = channels; a.silu = silu != 0;

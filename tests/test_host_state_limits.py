@@ -1,4 +1,4 @@
-"""The largest calls of rh_state_scan that one launch takes, and the next larger ones, which are refused before any work (no GPU; the recording
+"""The largest calls of rh_state_scan, rh_state_conv and rh_norm_gated that one launch takes, and the next larger ones, which are refused before any work (no GPU; the recording
 stand-in of test_host_calls takes the place of the HIP runtime, so nothing runs)."""
 from test_host_capture import run_child  # noqa: F401  (the fixture)
 from test_host_state import SETUP
@@ -40,4 +40,15 @@ for groups, blocks in ((65536, 65536), (32768, 32768), (1, 4096)):
     most = min(2048, MOST // blocks)
     assert taken(lambda: scan(rows(most, 5000), wide(65536, 128, groups), 65536)), groups
     if most < 2048: assert not taken(lambda: scan(rows(most + 1, 5000), wide(65536, 128, groups), 65536)), groups
+''')
+
+
+def test_convolution_and_norm(run_child):  # noqa: F811
+    run_child(WIDE + '''
+ch = 8192                                                                # 1024 pieces of bf16
+most = (2 ** 31 - 2 ** 12) // 1024
+assert taken(lambda: conv(rows(most), ch=ch, xs=ch, ys=ch)) and not taken(lambda: conv(rows(most + 1), ch=ch, xs=ch, ys=ch))
+assert taken(lambda: conv(rows(5, most * 16 - 80), ch=ch, xs=ch, ys=ch)) and not taken(lambda: conv(rows(5, most * 16 - 64), ch=ch, xs=ch, ys=ch))
+most = (2 ** 32 - 1) // 1024                                             # 8192 columns of bf16 in a group: 512 lanes with two pieces
+assert taken(lambda: gated(n=2 * most, cols=ch, groups=1, xs=ch, zs=ch)) and not taken(lambda: gated(n=2 * most + 2, cols=ch, groups=1, xs=ch, zs=ch))
 ''')
