@@ -1,4 +1,5 @@
-"""StreamPredictor.chunk on the GPU: offsets that do not fit the rows."""
+"""StreamPredictor.chunk on the GPU: offsets that do not fit the rows, and chunks so long that the scan cuts them."""
+import numpy as np
 import pytest
 import torch
 
@@ -39,3 +40,29 @@ def test_offsets_that_descend_or_leave_the_rows():
         assert bool((got[:lo] == 0).all()) and bool((got[hi:] == 0).all())
         assert torch.equal(a.lengths, b.lengths) and torch.equal(a.granted, b.granted)
         assert all(_off(p.double().cpu().numpy(), q.double().cpu().numpy()) <= BAR for p, q in zip(_states(a), _states(b)))
+
+
+@pytest.mark.parametrize("counts", [[300, 0, 287], [1, 700, 288]])
+def test_chunks_that_are_cut(counts):
+    """Streams of 288 frames and more, which the scan takes in pieces side by side: the scores and states that single steps give."""
+    cfg = _config(max_streams=3)
+    weights = P.random_weights(cfg, 7)
+    a, b = P.StreamPredictor(_rh(3), cfg, weights), P.StreamPredictor(_rh(3), cfg, weights, graph=True)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    for turn in range(2):
+        rows = torch.randn((sum(counts), cfg.n_features), generator=g, device="cuda")
+        offsets = np.concatenate(([0], np.cumsum(counts))).tolist()
+        got = a.chunk(rows, _i32(offsets))
+        want = torch.zeros_like(got)
+        for t in range(max(counts)):
+            live = [s for s in range(3) if t < counts[s]]
+            f = torch.zeros((3, cfg.n_features), device="cuda")
+            f[live] = rows[[offsets[s] + t for s in live]]
+            scores = b.step(f, _i32([int(t < n) for n in counts]))
+            for s in live:
+                want[offsets[s] + t] = scores[s]
+        off = ((got - want).flatten(1).norm(dim=1) / want.flatten(1).norm(dim=1)).cpu().numpy()
+        assert off.max() <= BAR, (turn, float(off.max()), int(off.argmax()))
+        assert torch.equal(a.lengths, b.lengths)
+        for p, q in zip(_states(a), _states(b)):
+            assert _off(p.double().cpu().numpy(), q.double().cpu().numpy()) <= BAR
