@@ -114,7 +114,7 @@ class StreamPredictor:
             # streams' states; what they hold of a stream that has not begun does not matter
             self.states = [(torch.zeros((n, cfg.taps - 1, cfg.inner), dtype=torch.bfloat16, device=dev), torch.zeros((n, cfg.inner, cfg.states), device=dev)) for _ in range(cfg.layers)]
             self.fade = [-torch.exp(self.norms[f"a_log{i}"]) for i in range(cfg.layers)]
-            self.every = torch.arange(n, **i32)
+            self.every, self.row = torch.arange(n, **i32), torch.zeros((0, 1), **i32)      # row: as many as a chunk has had
         else:
             self._make_caches(dev, i32)
         self.features, self.n_new = torch.zeros((n, cfg.n_features), device=dev), torch.zeros(n, **i32)
@@ -231,11 +231,14 @@ class StreamPredictor:
         if tuple(offsets.shape) != (streams + 1,) or offsets.dtype != torch.int32:
             raise ValueError(f"chunk: offsets {offsets.dtype} {tuple(offsets.shape)}, not torch.int32 {(streams + 1,)}")
         offsets = offsets.clamp(0, rows)
-        offsets.mul_((offsets[1:] >= offsets[:-1]).all())
+        begin, end, ends = offsets[:-1], offsets[1:], offsets[::streams]
+        offsets.mul_((end >= begin).all())
         scores = self._layers(features, self._state, self.every, offsets)
-        row = torch.arange(rows, dtype=torch.int32, device=offsets.device)
-        scores.masked_fill_(((row < offsets[0]) | (row >= offsets[-1]))[:, None, None], 0)   # their rows were never written
-        frames = offsets[1:] - offsets[:-1]
+        if self.row.shape[0] < rows:
+            self.row = torch.arange(rows, dtype=torch.int32, device=offsets.device).view(-1, 1)
+        ahead, behind = (self.row[:rows] < ends).unbind(1)          # of the first stream's rows, of the last one's end
+        scores.masked_fill_((ahead == behind).view(-1, 1, 1), 0)    # rows that were never written
+        frames = end - begin
         self.granted = frames > 0
         self.lengths.add_(frames)
         return scores
