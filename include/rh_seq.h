@@ -164,6 +164,8 @@ rh_status rh_state_conv(rh_ctx* ctx, const rh_state_rows* rows, const void* x, i
  *   state (dev, in/out) f32 [n_slots][channels][n].
  * Streams that are long for the call are cut into chunks, which are scanned side by side: from zeros first, for what each adds to the state
  * behind it, and again from the state that the chunks ahead leave.  Sums come in the same order every time.
+ * A row's power exp(delta * a) is held in 32 bits: 0 below exp(-87.3), infinite above exp(88.7).  An infinite state times that 0, and a state of 0 times that infinity, are no numbers, but
+ * infinite and 0 behind the end of a chunk where the power is that of all its rows; which rows those are goes by the streams of the call.
  * A launch takes 2^24 - 1 workgroups, each of 1024 / m channels, m being n rounded up to a power of two from 4 to 64: of four streams without offsets (8 channels of
  * more than 64 states), of one stream and one group with offsets (16 of more than 64 states).
  */

@@ -4,7 +4,8 @@
 // 920 rows, 2048 channels in bf16, inputs that no cache holds: 227 MB and 23 read twice in 51 us, 4.4 TB/s).
 // A thread has 16 bytes of channels and a run of rows, whose last inputs it keeps in registers.  Runs begin where streams do,
 // so that only a stream's first run looks at its state, and that thread, once it has read it, writes the state behind the last row:
-// no other thread reads or writes it, and it may be replaced in place.
+// no other thread writes it, and it may be replaced in place.  The last piece of a row that is no multiple of one is loaded from further ahead, with channels of the thread before, which may
+// have replaced them by then: row_place leaves them out, and has to.
 #include "seq_rows.h"
 #include "seq_streams.h"
 

@@ -4,6 +4,9 @@
 // neighbouring threads, with ITEMS pieces of 16 bytes a thread; pieces begin where groups do, at any address.  A row of more groups than the
 // threads are for goes ROUNDS times around.  The products stay in registers between the sums of squares, the largest |y| of the row and the output.
 // 27600 rows of 2048 in 8 groups of bf16, both outputs, inputs that no cache holds: 86 us, 4.6 TB/s; 14720 of 1540 in 4 groups of fp32 53, 5.1 TB/s; 8 of 2048, 8-bit output, 4.1.
+// A group's lanes are rounded up to a power of two, a row's threads too: in groups that do not fill them many threads have nothing.  bf16, 8-bit output: 20000 rows of 3 groups of 264 52 us, of 256
+// 22; 15000 of 16 of 72 36, of 64 18; 30000 of 520 28.5, of 512 19.5.  128 registers a thread are too few for fp32 groups of more than 16384 columns (19 spilled; 400 rows of 32768, both outputs,
+// 49 us, 3.5 TB/s), and for 4 rounds of 4 pieces in fp32 (12), of 2 in bf16 (20) and 16 rounds (2).
 // Several rows a workgroup, one after the other with the next one's loads ahead: 95 and 63 (two), 92 and 71 (four).
 #include "seq_rows.h"
 #include "seq_streams.h"

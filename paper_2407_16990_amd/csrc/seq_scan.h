@@ -6,11 +6,15 @@
 // Many tokens: bound by the vector instructions of h = exp2(delta a) h + delta x b, y += c h, of which the power takes twice as long as the four others: 24
 // cycles for a wave's 64 states.  A workgroup has CH channels of a stream and goes through its rows, ROWS of them staged in LDS at a time: delta and delta * x of every
 // channel, worked out once, b and c in fp32; the next rows' loads are in flight meanwhile.  y takes delta's place.  30 streams of 920 rows, 2048
-// channels of 16 states in bf16: 279 us, where the instructions of the recursion alone take 138 and the bytes 89.  A row of a workgroup's 64 channels takes each SIMD 138 cycles by
-// count, 94 of them in the recursion, the others mostly in softplus and SiLU; with eight workgroups a CU it takes 140, with the four that this call has 160.
+// channels of 16 states in bf16: 275 us, where the instructions of the recursion alone take 138 and the bytes 89.  A row of a workgroup's 64 channels takes each SIMD 140 cycles by
+// count, 94 of them in the recursion, the others mostly in softplus and SiLU.  A CU holds three workgroups (152 registers, 42 KB of LDS), so that the 960 of this call are a round of
+// 768 and a quarter of one, at 188 cycles a row and workgroup; one whole round and two (24 and 48 such streams, 193 and 373 us) are at 163 and 160.
 // (128 channels a workgroup 295 us where 64 took 286; 32 rows a stage 281, 16 329; registers for four waves a SIMD, some of them spilled, 290.)
 // Where streams are few, long ones are cut into chunks that are scanned side by side, twice: from zeros, for what they add to the state behind them, and
-// again from the state that those ahead leave.  16384 rows of one stream, 1024 channels: 77 us and 88.
+// again from the state that those ahead leave.  16384 rows of one stream, 1024 channels: 73 us and 89.  The first launch keeps room in LDS for c, which it does not read: three
+// workgroups a CU there too, where its registers would let five in.
+// A count of states between the powers of two costs what the next one does, and is masked besides: 30 streams of 250, 1024 channels, 16 states 46 us, 17 to 24 83, 32 73, 48 155, 64 123,
+// 65 to 96 340, 128 244.
 #pragma once
 // us, channels of 16 states in bf16 unless said otherwise.  SCAN_TARGET 2, 3, 4: 16384 rows of one stream, 1024 channels, 155, 160, 163; 37 of up to 2000, 522 of 13 in fp32, 240, 205, 217;
 // 8 of 600, 1024, 59.5, 52, 52; 8 of 1000, 1024 of 128, 240, 240, 348; 12 of up to 3000, 1024, 178, 157, 177.  SCAN_LEAST 128: one of 300, 1024, 33.1 for 21.7; one of 1000, 2048, 36.1 for 31.7.
@@ -499,8 +503,9 @@ __device__ __forceinline__ void scan_chunk(const scan_args& a, f32x4* s_stage, i
                     const f32x4 more = __builtin_bit_cast(f32x4, add[i]);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        // Step by step no power was 0 or infinite, whatever all of them make: in two halves, which neither are, an infinite state stays infinite,
-                        // one of zeros zero, and a small one may grow by more than 2^128.
+                        // As if no row's power were 0 or infinite, whatever all of them make: in two halves, which neither are, an infinite state stays infinite,
+                        // one of zeros zero, and a small one may grow by more than 2^128.  Where a row's own is, the rows one after the other make an infinite state, or one of
+                        // zeros, no number instead.
                         float f = __builtin_amdgcn_exp2f(0.5f * __uint_as_float(sum[i]) * fade[q][e]);
                         f = f == 0.f ? 0x1p-149f : f > FLT_MAX ? FLT_MAX : f;
                         v[e] = fmaf(f, f * v[e], more[e]);

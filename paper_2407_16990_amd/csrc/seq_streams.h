@@ -85,6 +85,7 @@ __device__ __forceinline__ int streams_find(const int32_t* s, int n, int32_t q)
     return lo;
 }
 
+// v / (1 + exp(-v)) within (|v| + 8) 2^-24 of itself: the power's argument is rounded once, and power and reciprocal are the hardware's
 __device__ __forceinline__ float seq_silu(float v) { return v * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(v * -1.44269504089f)); }
 
 // refusals of a call's rows; `name` is the call's
