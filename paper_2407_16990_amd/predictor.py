@@ -114,7 +114,7 @@ class StreamPredictor:
             # streams' states; what they hold of a stream that has not begun does not matter
             self.states = [(torch.zeros((n, cfg.taps - 1, cfg.inner), dtype=torch.bfloat16, device=dev), torch.zeros((n, cfg.inner, cfg.states), device=dev)) for _ in range(cfg.layers)]
             self.fade = [-torch.exp(self.norms[f"a_log{i}"]) for i in range(cfg.layers)]
-            self.every, self.row = torch.arange(n, **i32), torch.zeros((0, 1), **i32)      # row: as many as a chunk has had
+            self.every = torch.arange(n, **i32)
         else:
             self._make_caches(dev, i32)
         self.features, self.n_new = torch.zeros((n, cfg.n_features), device=dev), torch.zeros(n, **i32)
@@ -234,9 +234,9 @@ class StreamPredictor:
         begin, end, ends = offsets[:-1], offsets[1:], offsets[::streams]
         offsets.mul_((end >= begin).all())
         scores = self._layers(features, self._state, self.every, offsets)
-        if self.row.shape[0] < rows:
-            self.row = torch.arange(rows, dtype=torch.int32, device=offsets.device).view(-1, 1)
-        ahead, behind = (self.row[:rows] < ends).unbind(1)          # of the first stream's rows, of the last one's end
+        # made anew every time: one kept from a call that a caller captures would hold nothing until the graph's replay
+        row = torch.arange(rows, dtype=torch.int32, device=offsets.device)
+        ahead, behind = (row.view(-1, 1) < ends).unbind(1)          # of the first stream's rows, of the last one's end
         scores.masked_fill_((ahead == behind).view(-1, 1, 1), 0)    # rows that were never written
         frames = end - begin
         self.granted = frames > 0

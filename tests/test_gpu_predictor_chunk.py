@@ -66,3 +66,31 @@ def test_chunks_that_are_cut(counts):
         assert torch.equal(a.lengths, b.lengths)
         for p, q in zip(_states(a), _states(b)):
             assert _off(p.double().cpu().numpy(), q.double().cpu().numpy()) <= BAR
+
+
+def test_a_caller_may_capture_a_chunk():
+    """A chunk in a caller's graph, first of all its calls but one of the context's: replays with new rows and offsets are what the calls give, and so are calls between them."""
+    cfg = _config(max_streams=3)
+    weights = P.random_weights(cfg, 8)
+    rh, other = _rh(3), _rh(3)
+    a, b = P.StreamPredictor(rh, cfg, weights), P.StreamPredictor(other, cfg, weights)
+    g = torch.Generator(device="cuda").manual_seed(2)
+    rows, offsets = torch.zeros((400, cfg.n_features), device="cuda"), _i32([0, 350, 380, 400])
+    P.StreamPredictor(rh, cfg, weights).chunk(rows, offsets)        # the context's scratch memory is there
+    torch.cuda.synchronize()
+    side, main, graph = torch.cuda.Stream(), torch.cuda.current_stream(), torch.cuda.CUDAGraph()
+    rh.set_stream(side)
+    try:
+        with torch.cuda.graph(graph, stream=side):
+            scores = a.chunk(rows, offsets)
+    finally:
+        rh.set_stream(main)
+    for given in ([0, 350, 380, 400], [0, 20, 20, 390], [3, 390, 390, 390], [0, 9, 5, 400], [0, 1, 2, 400]):
+        new = torch.randn((400, cfg.n_features), generator=g, device="cuda")
+        few = torch.randn((5, cfg.n_features), generator=g, device="cuda")
+        rows.copy_(new)
+        offsets.copy_(_i32(given))
+        graph.replay()
+        assert torch.equal(scores, b.chunk(new, _i32(given)))
+        assert torch.equal(a.chunk(few, _i32([0, 2, 2, 4])), b.chunk(few, _i32([0, 2, 2, 4])))
+        assert torch.equal(a.lengths, b.lengths) and all(torch.equal(p, q) for p, q in zip(_states(a), _states(b)))
